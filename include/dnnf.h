@@ -48,7 +48,11 @@ typedef enum {
   DNNF_NOT_FINALIZED = -8
 } dnnf_status;
 
-typedef enum { DNNF_F32 = 0, DNNF_F16 = 1, DNNF_BF16 = 2, DNNF_I32 = 3, DNNF_I64 = 4, DNNF_BOOL = 5 } dnnf_dtype;
+/* I8 and U8 are the storage of quantised caches and weights (CacheWrite, CacheRead, CacheAttention, MatMulInt4);
+ * other operators refuse them. */
+typedef enum {
+  DNNF_F32 = 0, DNNF_F16 = 1, DNNF_BF16 = 2, DNNF_I32 = 3, DNNF_I64 = 4, DNNF_BOOL = 5, DNNF_I8 = 6, DNNF_U8 = 7
+} dnnf_dtype;
 typedef enum { DNNF_INPUT = 0, DNNF_WEIGHT = 1, DNNF_INTERMEDIATE = 2, DNNF_OUTPUT = 3 } dnnf_tensor_kind;
 
 /* Mapping types of Sec. 3.1, numbered in the increasing order of complexity
@@ -90,7 +94,37 @@ dnnf_status dnnf_graph_add_tensor(dnnf_graph* g, const char* name, dnnf_dtype dt
 dnnf_status dnnf_graph_set_const(dnnf_graph* g, int tensor_id, const double* values, int64_t count);
 
 /* Appends an operator of ONNX kind `op_kind` ("Conv", "MatMul", "Add", ...; Table 2 vocabulary).
- * in_ids/out_ids: host arrays of tensor handles.  op_id receives the operator handle. */
+ * in_ids/out_ids: host arrays of tensor handles.  op_id receives the operator handle.
+ *
+ * Beside the ONNX kinds there are four of single-token inference.
+ *
+ * Three deal with a key / value cache kept in pages.  A pool is [P pages, HK key heads, S slots, channels], one for keys and one
+ * for values (P, HK and S alike; channels a multiple of 16, at most 256, and not necessarily alike), in a float type or in
+ * I8.  `table` [B, M] (I32) names each sequence's pages: position p of sequence b is slot p % S of page table[b][p / S].  An entry
+ * outside [0, P) is a page that is not there: its rows are neither written nor seen.  Pools of I8 come with scales
+ * [P, HK, S] (F32): a row is its scale times whole numbers in [-127, 127], scale = max |x| / 127, the numbers x / scale
+ * rounded to nearest, halves to even; a row that lies wholly below 2^-119 is kept as zeros, one with an infinity or NaN reads
+ * back as NaN.  [..] marks the operands that come with I8.
+ *   CacheWrite (k_pool, v_pool, [k_scale, v_scale,] k, v, table, first [, count]) -> k_pool, v_pool [, k_scale, v_scale]
+ *       Token t of sequence b in k, v [B, T, HK, channels] becomes position first[b] + t, for t below count[b] (an operand that may
+ *       be left out: T); positions below 0 or behind the table's M * S are left out.  The pools are INPUT tensors, updated in
+ *       place: the results are OUTPUT tensors that take the same pointers at run time (anything else is refused), and other
+ *       operators read the results.  All other rows stay as they are.  A slot written twice in one call keeps the last row
+ *       (by sequence, then by token).
+ *   CacheRead (k_pool, v_pool, [k_scale, v_scale,] table, held) -> k, v     attribute "length" = L
+ *       Positions 0 .. L - 1 laid out as [B, L, HK, channels]; zeros from held[b] on and where no page is.
+ *   CacheAttention (q, k_pool, v_pool, [k_scale, v_scale,] table, held) -> o     attributes "scale", "window"
+ *       One new token per sequence: q [B, HQ, channels of a key] -> [B, HQ, channels of a value], HQ a multiple of HK (query head
+ *       h reads key head h / (HQ / HK)).  Softmax(scale q K^T) V over positions 0 .. held[b] - 1 (the last "window" of them if that
+ *       is above 0); scale is 1 / sqrt(channels of a key) unless given.  Without any key, or with scores of -infinity alone, the
+ *       result is zeros.  held is taken within [0, M * S].  Slots that are not read may hold anything, NaN included.
+ * q, k, v and o are of the pools' type, of any float type if the pools are I8.
+ *
+ *   MatMulInt4 (x, w, scale [, zero]) -> y     attribute "group_size" = G, a multiple of 32
+ *       y [.., N] = sum over k of x [.., K] times (code[n, k] - zero[n, k / G]) * scale[n, k / G].  w is U8 [N, (K + 1) / 2], two codes a
+ *       byte, the even k in the low half; scale [N, groups of K] is of x's type, zero U8 of that shape (8 where it is left
+ *       out).  x has rank 2 or more and is finite (an infinity or NaN makes its row NaN).  One-to-One operators, Reshapes and
+ *       Splits behind the product run in its kernel, as behind MatMul. */
 dnnf_status dnnf_graph_add_op(dnnf_graph* g, const char* op_kind, int n_in, const int* in_ids, int n_out,
                               const int* out_ids, const dnnf_attr* attrs, int n_attrs, int* op_id);
 
@@ -212,7 +246,9 @@ typedef struct {
                               AveragePool), 2 MFMA GEMM (MatMul / Gemm / Einsum), 3 convolution as implicit GEMM
                               (Conv 2-d / 3-d, ConvTranspose), 4 depthwise convolution, 5 alias (a lone contiguous
                               Reshape or a stacking Concat: no kernel, the result shares its operands' storage), 6 streaming-softmax
-                              attention (opts.attention), 7 squeeze-excite tail (opts.squeeze_excite) */
+                              attention (opts.attention), 7 squeeze-excite tail (opts.squeeze_excite),
+                              8 key / value cache (CacheWrite, CacheRead, CacheAttention), 9 MFMA product with weights of
+                              four bits (MatMulInt4) */
   double bytes;            /* algorithmic HBM bytes: external inputs read once + outputs written once */
   double flops;
   double irs_bytes_removed;/* intermediate results that never reach HBM (Table 5's IRS statistic) */
@@ -254,7 +290,8 @@ dnnf_status dnnf_plan_prepare(dnnf_plan* p, void* workspace, void* stream);
  * input_dev_ptrs / output_dev_ptrs: host arrays of device pointers, one per INPUT / OUTPUT tensor
  * in declaration order.  With opts.graphs = 1 the second call with the same pointers records the
  * launches into a HIP graph (on a stream the plan owns) and that call and later ones enqueue the graph
- * on `stream` instead; the buffers' contents are read when the graph runs, as with plain launches. */
+ * on `stream` instead; the buffers' contents are read when the graph runs, as with plain launches.  Calls that may overlap
+ * (two streams, two captured graphs) need a workspace each: it holds what passes between the kernels of one call. */
 dnnf_status dnnf_plan_run(dnnf_plan* p, const void* const* input_dev_ptrs, void* const* output_dev_ptrs,
                           void* workspace, void* stream);
 /* dnnf_plan_run for callers that cannot allocate device memory or hand over a workspace: code under HIP graph

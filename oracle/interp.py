@@ -26,6 +26,90 @@ from scipy import special as _sp
 F64 = np.float64
 
 
+# ------------------------------------------------------------------ single-token inference (not in the paper)
+# A pool is [pages, key heads, slots of a page, channels]; position p of sequence b is slot p % S of page table[b, p // S].  Rows on
+# pages that the table does not name are neither written nor seen.  With scales, a pool holds whole numbers of a row's step.
+def _slots(table, b, lo, hi, pages, S):
+    """[(position, page, slot)] of sequence b's positions in [lo, hi) that are there."""
+    rows = [(p, int(table[b, p // S]), p % S) for p in range(max(lo, 0), min(hi, table.shape[1] * S))]
+    return [r for r in rows if 0 <= r[1] < pages]
+
+
+def _quantised(x):
+    """(whole numbers, step) of rows along the last axis.  The step is kept in 32 bits and both quotients are taken there:
+    which of two whole numbers a value at their middle becomes belongs to the definition."""
+    x = x.astype(np.float32)
+    top = np.max(np.abs(x), axis=-1)
+    with np.errstate(all="ignore"):
+        step = np.where(top < np.float32(2.0 ** -119), np.float32(0), (top / np.float32(127)).astype(np.float32))
+        step = np.where(np.all(np.isfinite(x), axis=-1), step, np.float32(np.nan))
+        n = np.where(step[..., None] > 0, np.rint((x / step[..., None]).astype(np.float32)), np.float32(0))
+    return n.astype(F64), step.astype(F64)
+
+
+def _cache_write(ins, attrs):
+    scaled = ins[2].ndim == 3
+    pools = [np.array(t, dtype=F64) for t in ins[:4 if scaled else 2]]
+    k, v, table, first = ins[len(pools):len(pools) + 4]
+    count = ins[len(pools) + 4] if len(ins) > len(pools) + 4 else np.full(len(first), k.shape[1])
+    for b in range(len(first)):
+        f, n = int(first[b]), min(max(int(count[b]), 0), k.shape[1])
+        for p, page, slot in _slots(table, b, f, f + n, pools[0].shape[0], pools[0].shape[2]):
+            for i, x in enumerate((k, v)):
+                row = x[b, p - f]
+                if scaled:
+                    row, pools[2 + i][page, :, slot] = _quantised(row)
+                pools[i][page, :, slot] = row
+    return pools
+
+
+def _cache_rows(pools, i, page, slot):
+    x = pools[i][page, :, slot].astype(F64)
+    return x * pools[2 + i][page, :, slot][:, None] if len(pools) == 4 else x
+
+
+def _cache_read(ins, attrs):
+    pools, (table, held) = ins[:-2], ins[-2:]
+    L, out = int(attrs["length"]), []
+    for i in range(2):
+        y = np.zeros((len(held), L, pools[i].shape[1], pools[i].shape[3]), dtype=F64)
+        for b in range(len(held)):
+            for p, page, slot in _slots(table, b, 0, min(int(held[b]), L), pools[0].shape[0], pools[0].shape[2]):
+                y[b, p] = _cache_rows(pools, i, page, slot)
+        out.append(y)
+    return out
+
+
+def _cache_attention(ins, attrs):
+    q, pools, (table, held) = ins[0], ins[1:-2], ins[-2:]
+    B, HQ, D = q.shape
+    HK, window, scale = pools[0].shape[1], int(attrs.get("window", 0)), float(attrs.get("scale", 1.0 / np.sqrt(D)))
+    out = np.zeros((B, HQ, pools[1].shape[3]), dtype=F64)
+    for b in range(B):
+        end = min(int(held[b]), table.shape[1] * pools[0].shape[2])
+        rows = _slots(table, b, end - window if window > 0 else 0, end, pools[0].shape[0], pools[0].shape[2])
+        if not rows:
+            continue
+        k, v = (np.stack([_cache_rows(pools, i, page, slot) for _, page, slot in rows]) for i in range(2))      # [keys, HK, D]
+        for h in range(HQ):
+            s = k[:, h * HK // HQ] @ q[b, h] * scale
+            p = np.exp(s - s.max())
+            out[b, h] = p @ v[:, h * HK // HQ] / p.sum()
+    return out
+
+
+_CACHE = {"CacheWrite": _cache_write, "CacheRead": _cache_read, "CacheAttention": _cache_attention}
+
+
+def _matmul_int4(ins, attrs):
+    x, w, scale = ins[:3]
+    K, G = x.shape[-1], int(attrs["group_size"])
+    k = np.arange(K)
+    code = (w[:, k // 2].astype(np.int64) >> (4 * (k % 2))) & 15
+    zero = ins[3][:, k // G] if len(ins) > 3 else 8
+    return x @ ((code - zero) * scale[:, k // G]).T
+
+
 # ------------------------------------------------------------------ elementwise (One-to-One, Table 2)
 def _clip(x, attrs):
     return np.minimum(np.maximum(x, attrs.get("min", -np.inf)), attrs.get("max", np.inf))
@@ -364,6 +448,10 @@ def eval_op(kind, ins, attrs):
             if int(sc) != 1:
                 y = np.repeat(y, int(sc), axis=ax)
         return y
+    if kind in ("CacheWrite", "CacheRead", "CacheAttention"):
+        return _CACHE[kind](ins, attrs)
+    if kind == "MatMulInt4":
+        return _matmul_int4(ins, attrs)
     raise NotImplementedError(f"oracle: operator {kind}")
 
 
@@ -380,7 +468,7 @@ def run_graph(spec, feeds=None, keep=None):
             src = feeds[t.name] if feeds and t.name in feeds else t.data
             if src is None:
                 raise ValueError(f"no data for {t.name}")
-            env[t.name] = np.asarray(src).astype(np.int64 if t.dtype in ("i32", "i64") else F64)
+            env[t.name] = np.asarray(src).astype(np.int64 if t.dtype in ("i32", "i64", "i8", "u8") else F64)
     outs = {t.name for t in spec.tensors.values() if t.kind == "output"}
     want = set(spec.tensors) if keep == "all" else outs | set(keep or ())
     uses = {}

@@ -15,11 +15,11 @@ import numpy as np
 from . import _lib
 from ._lib import Attr, BlockInfo, PlanOpts, RewriteStats
 
-DTYPES = {"f32": 0, "f16": 1, "bf16": 2, "i32": 3, "i64": 4, "bool": 5}
+DTYPES = {"f32": 0, "f16": 1, "bf16": 2, "i32": 3, "i64": 4, "bool": 5, "i8": 6, "u8": 7}
 KINDS = {"input": 0, "weight": 1, "intermediate": 2, "output": 3}
 MAPPING_NAMES = ["One-to-One", "Reorganize", "Shuffle", "One-to-Many", "Many-to-Many"]
 COLOUR_NAMES = ["green", "yellow", "red"]
-FAMILY_NAMES = ["elementwise", "row-reduction", "gemm", "conv", "depthwise-conv", "alias", "attention", "squeeze-excite"]
+FAMILY_NAMES = ["elementwise", "row-reduction", "gemm", "conv", "depthwise-conv", "alias", "attention", "squeeze-excite", "cache", "int4-gemm"]
 
 
 class DnnfError(RuntimeError):
@@ -223,6 +223,10 @@ class Plan:
     def run(self, inputs, outputs, workspace: int, stream: int = 0):
         _check(_lib.lib().dnnf_plan_run(self._h, self._ptrs(inputs), self._ptrs(outputs), workspace or None, stream or None))
 
+    def bind(self, inputs, outputs, workspace: int) -> "BoundPlan":
+        """The plan with its buffers fixed: a loop of small calls marshals the pointers once.  The buffers must outlive the result."""
+        return BoundPlan(self, inputs, outputs, workspace)
+
     def run_static(self, inputs, outputs, stream: int = 0):
         _check(_lib.lib().dnnf_plan_run_static(self._h, self._ptrs(inputs), self._ptrs(outputs), stream or None))
 
@@ -247,6 +251,18 @@ class Plan:
             d["ops"] = [self.op_kind(i) for i in self.block_ops(b)]
             out.append(d)
         return out
+
+
+class BoundPlan:
+    """A plan and the buffers it runs on (Plan.bind)."""
+
+    def __init__(self, plan: Plan, inputs, outputs, workspace: int):
+        self._plan = plan
+        self._args = (plan._h, plan._ptrs(inputs), plan._ptrs(outputs), C.c_void_p(workspace or None))
+        self._run = _lib.lib().dnnf_plan_run
+
+    def run(self, stream: int = 0):
+        _check(self._run(*self._args, stream or None))
 
 
 def precompile_spec(spec, fusion=1, rewrite=True, cache_dir=None, tune=0, attention=0, layout=0, broadcast_prologue=0, gemm_norm=0, squeeze_excite=0) -> int:
@@ -277,13 +293,13 @@ class Session:
         self.guard_bytes = int(guard_bytes)
         assert self.guard_bytes % 256 == 0
         self._guards = []
-        tdt = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i32": torch.int32, "i64": torch.int64, "bool": torch.bool}
+        tdt = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i32": torch.int32, "i64": torch.int64, "bool": torch.bool, "i8": torch.int8, "u8": torch.uint8}
         self.graph, self.ids = graph_from_spec(spec)
         self.rewrite_stats = self.graph.rewrite() if rewrite else None
 
         def up(t):
             a = t.data
-            if t.dtype in ("i32", "i64", "bool"):
+            if t.dtype in ("i32", "i64", "bool", "i8", "u8"):
                 return torch.from_numpy(np.ascontiguousarray(a)).to(tdt[t.dtype]).to(self.device)
             return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(self.device).to(tdt[t.dtype]).contiguous()
 
@@ -291,7 +307,11 @@ class Session:
         self.n_sets = n_buffer_sets
         self.inputs = [[up(t) for t in spec.tensors.values() if t.kind == "input"] for _ in range(n_buffer_sets)]
         self.out_specs = [t for t in spec.tensors.values() if t.kind == "output"]
-        self.outputs = [[self._alloc(t.shape, tdt[t.dtype]) for t in self.out_specs] for _ in range(n_buffer_sets)]
+        # what CacheWrite updates in place is an input and an output in one buffer
+        in_at = {t.name: i for i, t in enumerate(t for t in spec.tensors.values() if t.kind == "input")}
+        same = {o: in_at[i] for op in spec.ops if op.kind == "CacheWrite" for i, o in zip(op.inputs, op.outputs)}
+        self.outputs = [[self.inputs[k][same[t.name]] if t.name in same else self._alloc(t.shape, tdt[t.dtype]) for t in self.out_specs]
+                        for k in range(n_buffer_sets)]
         self.stream = torch.cuda.current_stream(self.device).cuda_stream
         scratch = None
         if profile:

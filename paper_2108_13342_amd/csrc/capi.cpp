@@ -53,7 +53,7 @@ dnnf_status dnnf_graph_add_tensor(dnnf_graph* g, const char* name, dnnf_dtype dt
                                   dnnf_tensor_kind kind, int* tensor_id) {
   return guard([&] {
     REQUIRE(g && name && tensor_id && rank >= 0 && rank <= 8 && (rank == 0 || dims), "bad argument to dnnf_graph_add_tensor");
-    REQUIRE(dtype >= DNNF_F32 && dtype <= DNNF_BOOL && kind >= DNNF_INPUT && kind <= DNNF_OUTPUT, "bad dtype or kind");
+    REQUIRE(dtype >= DNNF_F32 && dtype <= DNNF_U8 && kind >= DNNF_INPUT && kind <= DNNF_OUTPUT, "bad dtype or kind");
     *tensor_id = g->g.add_tensor(name, dtype, Dims(dims, dims + rank), kind);
   });
 }
@@ -170,7 +170,7 @@ dnnf_status dnnf_graph_rewrite(dnnf_graph* g, dnnf_rewrite_stats* stats) {
 dnnf_status dnnf_graph_dump_json(const dnnf_graph* g, char* buf, size_t cap, size_t* needed) {
   return guard([&] {
     REQUIRE(g, "null graph");
-    static const char* dts[] = {"f32", "f16", "bf16", "i32", "i64", "bool"};
+    static const char* dts[] = {"f32", "f16", "bf16", "i32", "i64", "bool", "i8", "u8"};
     static const char* kinds[] = {"input", "weight", "intermediate", "output"};
     std::string s = "{\"tensors\":[";
     char num[64];
@@ -321,7 +321,7 @@ dnnf_status dnnf_plan_dump_json(const dnnf_plan* p, char* buf, size_t cap, size_
   return guard([&] {
     REQUIRE(p, "null plan");
     const Plan& P = *p->p;
-    static const char* dts[] = {"f32", "f16", "bf16", "i32", "i64", "bool"};
+    static const char* dts[] = {"f32", "f16", "bf16", "i32", "i64", "bool", "i8", "u8"};
     static const char* kinds[] = {"input", "weight", "intermediate", "output"};
     auto tensor = [&](int t) {
       int root = t;

@@ -82,6 +82,12 @@ static const std::vector<OpKindInfo> kOpKinds = {
     {"MatMul", OC_MATMUL, DNNF_MANY_TO_MANY, false, false, false, false, 0},
     {"GlobalAveragePool", OC_GAP, DNNF_MANY_TO_MANY, false, false, false, false, 0},
     {"Normalize", OC_NORMALIZE, DNNF_MANY_TO_MANY, false, false, false, false, 0},
+    // ---- single-token inference (decode_ops.cpp): a key / value cache in pages, and weights of four bits.  A row that is
+    //      read back lands in one place, but which one a run-time table says, as a Gather's: One-to-Many.
+    {"CacheWrite", OC_CACHE_WRITE, DNNF_MANY_TO_MANY, false, false, false, false, 0},
+    {"CacheRead", OC_CACHE_READ, DNNF_ONE_TO_MANY, false, false, false, false, 0},
+    {"CacheAttention", OC_CACHE_ATTN, DNNF_MANY_TO_MANY, false, false, false, false, 0},
+    {"MatMulInt4", OC_MATMUL_INT4, DNNF_MANY_TO_MANY, false, false, false, false, 0},
 };
 
 const std::vector<OpKindInfo>& all_op_kinds() { return kOpKinds; }
@@ -467,6 +473,8 @@ Dims infer_shape(const Graph& g, const Op& op, int oi) {
       }
       return out;
     }
+    case OC_CACHE_WRITE: case OC_CACHE_READ: case OC_CACHE_ATTN: case OC_MATMUL_INT4:
+      return infer_decode_shape(g, op, oi);
     default:
       throw Error(DNNF_UNSUPPORTED_OP, "operator " + op.kind + " is classified but cannot be executed");
   }
@@ -517,6 +525,11 @@ double op_flops(const Graph& g, const Op& op) {
     case OC_GEMM: {
       const Dims& a = g.tensors[op.in[0]].dims;
       return 2.0 * on * (double)(op.i("transA", 0) ? a[0] : a[1]);
+    }
+    case OC_MATMUL_INT4: return 2.0 * on * (double)g.tensors[op.in[0]].dims.back();
+    case OC_CACHE_ATTN: {        // at the table's capacity (how many keys a sequence holds is known when it runs)
+      const CacheOperands c = cache_operands(g, op);
+      return 2.0 * (double)(c.B * c.HQ * c.M * c.S) * (double)(c.D[0] + c.D[1]);
     }
     default: {
       double tot = 0;
@@ -584,6 +597,11 @@ void Graph::finalize() {
   for (auto& op : ops) {
     if (!op.alive) continue;
     DNNF_CHECK(!op.out.empty(), DNNF_INVALID_ARG, op.kind + ": no outputs");
+    if (!is_decode_op(op))
+      for (auto* side : {&op.in, &op.out})
+        for (int t : *side)
+          DNNF_CHECK(tensors[t].dtype != DNNF_I8 && tensors[t].dtype != DNNF_U8, DNNF_UNSUPPORTED_OP,
+                     op.kind + ": tensors of 8 bits are operands of the cache operators and of MatMulInt4 only");
     for (size_t k = 0; k < op.out.size(); k++) {
       Dims want = infer_shape(*this, op, (int)k);
       const Tensor& t = tensors[op.out[k]];
@@ -614,6 +632,8 @@ void Graph::finalize() {
     }
   }
   relink();
+  for (auto& op : ops)
+    if (op.alive && is_decode_op(op)) check_decode_op(*this, op);
   finalized = true;
 }
 

@@ -64,6 +64,10 @@ enum OpClass {
   OC_EXPAND,
   OC_RESIZE,     // Resize / Upsample, nearest neighbour by integer factors ("scales", one per axis)
   OC_D2S,        // DepthToSpace / SpaceToDepth (classified only)
+  OC_CACHE_WRITE,  // rows of new keys / values into the pages of a cache, in place
+  OC_CACHE_READ,   // rows of a cache laid out densely
+  OC_CACHE_ATTN,   // one new token per sequence attending over a cache
+  OC_MATMUL_INT4,  // x times weights of four bits with a scale (and a zero point) per group of the contraction
   OC_OTHER       // classified by Table 2, not executable here
 };
 
@@ -153,6 +157,19 @@ struct Graph {
 };
 
 Dims infer_shape(const Graph& g, const Op& op, int out_index);
+
+// The operators of single-token inference (decode_ops.cpp).  Operands of a cache operator by their meaning, with the
+// extents that its shapes agree on; -1 where the operator has no such operand.
+struct CacheOperands {
+  int q = -1, pool[2] = {-1, -1}, scale[2] = {-1, -1}, fresh[2] = {-1, -1}, table = -1, first = -1, count = -1, held = -1;
+  int64_t P = 0, HK = 0, S = 0, D[2] = {0, 0};      // pages, key heads, slots of a page, channels of a key / a value
+  int64_t B = 0, M = 0, T = 0, HQ = 0;              // sequences, pages of a table row, new tokens, query heads
+  bool eight_bits = false;
+};
+bool is_decode_op(const Op& op);
+CacheOperands cache_operands(const Graph& g, const Op& op);
+Dims infer_decode_shape(const Graph& g, const Op& op, int out_index);
+void check_decode_op(const Graph& g, const Op& op);      // types, attributes, and what may share storage (a relinked graph)
 Dims broadcast_dims(const Dims& a, const Dims& b);
 int classify_op(const Graph& g, const Op& op);      // Table 2 + most-complex-pair rule
 double op_flops(const Graph& g, const Op& op);      // cost model of Sec. 4.2

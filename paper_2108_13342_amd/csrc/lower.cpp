@@ -995,6 +995,7 @@ Lowered lower_block(const Graph& g, const Block& b, const LowerOpts& o) {
     const Op& op = g.ops[oi];
     switch (op.info->cls) {
       case OC_CONV: case OC_CONVT: case OC_MATMUL: case OC_GEMM: case OC_REDUCE: case OC_SOFTMAX: case OC_NORMALIZE: case OC_GAP: case OC_POOL: case OC_SCAN:
+      case OC_CACHE_WRITE: case OC_CACHE_READ: case OC_CACHE_ATTN: case OC_MATMUL_INT4:
         anchors++;
         c.anchor_op = oi;
         c.anchor_out = op.out[0];
@@ -1183,6 +1184,8 @@ Lowered lower_block(const Graph& g, const Block& b, const LowerOpts& o) {
       case OC_SCAN: L = lower_scan(c); break;
       case OC_CONVT: L = lower_conv_transpose(c); break;
       case OC_MATMUL: case OC_GEMM: L = lower_gemm(c); break;
+      case OC_CACHE_WRITE: case OC_CACHE_READ: case OC_CACHE_ATTN: L = lower_cache(c); break;
+      case OC_MATMUL_INT4: L = lower_int4(c); break;
       default: L = lower_reduce(c); break;
     }
   }

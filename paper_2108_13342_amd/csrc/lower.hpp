@@ -19,7 +19,7 @@ struct Block {
   bool weight_only = false;  // computed once at prepare time
 };
 
-enum Family { FAM_EW = 0, FAM_REDUCE = 1, FAM_GEMM = 2, FAM_CONV = 3, FAM_DWCONV = 4, FAM_ALIAS = 5, FAM_ATTENTION = 6, FAM_SE = 7 };
+enum Family { FAM_EW = 0, FAM_REDUCE = 1, FAM_GEMM = 2, FAM_CONV = 3, FAM_DWCONV = 4, FAM_ALIAS = 5, FAM_ATTENTION = 6, FAM_SE = 7, FAM_CACHE = 8, FAM_INT4 = 9 };
 
 struct Launch {
   std::string name;       // kernel symbol
@@ -37,6 +37,7 @@ struct Lowered {
   int alias_src = -1, alias_dst = -1;  // FAM_ALIAS: dst shares src's storage
   // FAM_ALIAS of a stacking Concat: each listed tensor lives inside alias_dst's storage at the given byte offset
   std::vector<std::pair<int, int64_t>> alias_parts;
+  std::vector<std::pair<int, int>> in_place;   // (result, operand): the result is the operand's storage, updated
   int64_t scratch_bytes = 0;         // device memory the block's launches pass partial results through
   double bytes = 0, flops = 0, irs_removed = 0;
   std::string variant;               // human-readable template choice

@@ -1,0 +1,610 @@
+// Kernels of a key / value cache kept in pages: rows written in place, rows laid out densely, and the attention of one new
+// token per sequence over the rows it holds.
+//
+// A pool is [pages, key heads, slots, channels]: the rows of one head in one page lie one behind another, so a workgroup
+// that walks a head's keys reads runs of slots * channels elements.  Position p of sequence b is slot p % S of page
+// table[b][p / S].  Rows are numbered (page * HK + h) * S + slot in 32 bits (checked when the graph is finalised); their
+// elements are addressed in 64.  What the run-time tables say is bounded in the kernels: a table entry outside the pool is
+// a page that is not there (its rows are neither written nor seen), positions and counts are clamped to what the table and
+// the operands hold.
+//
+// Pools of 8 bits keep a row as whole numbers of a step of its own: step = max |x| / 127 in fp32, value = step * n with
+// n = x / step rounded to the nearest whole number, halves to even - at most half a step off.
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <sstream>
+
+#include "lower_ctx.hpp"
+
+namespace dnnf {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ CacheWrite
+const char* kWriteBody = R"KRN(
+#define VEC (16 / (int)sizeof(elem_t))
+#define VECTORS(D) ((D) / VEC)
+typedef elem_t in_t __attribute__((ext_vector_type(VEC)));
+typedef pool_t out_t __attribute__((ext_vector_type(VEC)));
+
+// positions [lo, hi) that sequence b writes
+DEV void written(const int b, const int* __restrict__ first, const int* __restrict__ fresh, int& f, int& lo, int& hi) {
+  f = first[b];
+  const int n = HAS_COUNT ? min(max(fresh[b], 0), TOKENS) : TOKENS;
+  lo = max(f, 0);
+  hi = (int)min((long long)f + n, (long long)TABLE * SLOTS);
+}
+// the page that entry e of all sequences' written pages lies in; -1: nothing is written there
+DEV int written_page(const int e, const int* __restrict__ table, const int* __restrict__ first, const int* __restrict__ fresh, int& lo, int& hi, int& p0) {
+  const int b = e / SPANS;
+  int f;
+  written(b, first, fresh, f, lo, hi);
+  if (lo >= hi) return -1;
+  const int lp = lo / SLOTS + e % SPANS;
+  p0 = lp * SLOTS;
+  return p0 < hi ? table[(long long)b * TABLE + lp] : -1;
+}
+
+template <int D> DEV void put(pool_t* __restrict__ pool, float* __restrict__ scale, const elem_t* __restrict__ x, const long long src, const long long dst, const int lane) {
+  const bool on = lane < VECTORS(D);
+  in_t v = 0;
+  if (on) v = *(const in_t*)(x + src * D + lane * VEC);
+#if EIGHT_BITS
+  float f[VEC];
+  u32 top = 0;                                     // the largest magnitude, by bits: infinities and NaN lie above all others
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) { f[e] = cvt_in(v[e]); top = max(top, __builtin_bit_cast(u32, f[e]) & 0x7fffffffu); }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (u32)__shfl_xor((int)top, o, 64));
+  // a row with an infinity or NaN reads back as NaN; one that lies wholly below 2^-119 (where the step would leave the
+  // normal numbers) as zeros
+  float step = __builtin_bit_cast(float, top) / 127.0f;
+  if (top < 0x04000000u) step = 0.0f;
+  if (top >= 0x7f800000u) step = __builtin_nanf("");
+  out_t q;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) q[e] = (pool_t)(step > 0.0f ? __builtin_rintf(f[e] / step) : 0.0f);
+  if (on) *(out_t*)(pool + dst * D + lane * VEC) = q;
+  if (lane == 0) scale[dst] = step;
+#else
+  if (on) *(out_t*)(pool + dst * D + lane * VEC) = v;
+#endif
+}
+
+// A workgroup writes CHUNK positions that lie in one page, for every head; LANES lanes a row.  Where one slot is written
+// twice in a call the last write stays (sequences in order, then tokens): a workgroup looks through the written pages behind
+// its own for the same page - once, and row by row only if there is one.
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  __shared__ int clash;
+  const int tid = threadIdx.x, unit = blockIdx.x;
+  const int entry = unit / SUBS, b = entry / SPANS;
+  int f, lo, hi;
+  written(b, first, count, f, lo, hi);
+  if (lo >= hi) return;
+  const int lp = lo / SLOTS + entry % SPANS;
+  if (lp >= TABLE) return;
+  const int p0 = max(lo, lp * SLOTS + unit % SUBS * CHUNK), p1 = min(hi, min(lp * SLOTS + (unit % SUBS + 1) * CHUNK, (lp + 1) * SLOTS));
+  if (p0 >= p1) return;
+  const int page = table[(long long)b * TABLE + lp];
+  if ((u32)page >= (u32)PAGES) return;
+  if (tid == 0) clash = 0;
+  __syncthreads();
+  bool same = false;
+  for (int e = entry + 1 + tid; e < SEQUENCES * SPANS; e += 256) {
+    int l, h, p;
+    same |= written_page(e, table, first, count, l, h, p) == page;
+  }
+  if (same) clash = 1;
+  __syncthreads();
+  const int lane = tid % LANES;
+  for (int r = tid / LANES; r < (p1 - p0) * HEADS; r += 256 / LANES) {
+    const int p = p0 + r / HEADS, h = r % HEADS;
+    if (clash) {
+      bool later = false;
+      for (int e = entry + 1; e < SEQUENCES * SPANS && !later; ++e) {
+        int l, hh, q0;
+        if (written_page(e, table, first, count, l, hh, q0) == page) later = q0 + p % SLOTS >= l && q0 + p % SLOTS < hh;
+      }
+      if (later) continue;
+    }
+    const long long src = ((long long)b * TOKENS + (p - f)) * HEADS + h, dst = ((long long)page * HEADS + h) * SLOTS + p % SLOTS;
+    put<DK>(k_pool, k_scale, k, src, dst, lane);
+    put<DV>(v_pool, v_scale, v, src, dst, lane);
+  }
+}
+)KRN";
+
+// ------------------------------------------------------------------------------------------------ CacheRead
+const char* kReadBody = R"KRN(
+#define VEC (16 / (int)sizeof(elem_t))
+#define PER 4                                      // vectors of keys and of values that a thread has in flight
+typedef elem_t out_t __attribute__((ext_vector_type(VEC)));
+typedef pool_t in_t __attribute__((ext_vector_type(VEC)));
+
+template <int D> DEV void get(elem_t* __restrict__ out, const pool_t* __restrict__ pool, const float* __restrict__ scale,
+                              const int* __restrict__ table, const int* __restrict__ held) {
+  const idx_t total = (idx_t)SEQUENCES * LENGTH * HEADS * (D / VEC);
+  const idx_t base = (idx_t)blockIdx.x * (256 * PER) + threadIdx.x;
+  if (base >= total) return;
+  in_t x[PER];
+  float s[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const idx_t i = base + u * 256;
+    x[u] = 0;
+    s[u] = 0.0f;
+    if (i >= total) continue;
+    const idx_t row = i / (D / VEC);
+    const int v = (int)(i % (D / VEC)), h = (int)(row % HEADS), t = (int)(row / HEADS % LENGTH), b = (int)(row / HEADS / LENGTH);
+    if (t >= min(held[b], TABLE * SLOTS)) continue;
+    const int page = table[(long long)b * TABLE + t / SLOTS];
+    if ((u32)page >= (u32)PAGES) continue;
+    const long long r = ((long long)page * HEADS + h) * SLOTS + t % SLOTS;
+    x[u] = *(const in_t*)(pool + r * D + v * VEC);
+#if EIGHT_BITS
+    s[u] = scale[r];
+#endif
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const idx_t i = base + u * 256;
+    if (i >= total) continue;
+    out_t o;
+#if EIGHT_BITS
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { elem_t y; cvt_out(&y, (float)x[u][e] * s[u]); o[e] = y; }
+#else
+    o = x[u];
+#endif
+    dn_store_stream((out_t*)out + i, o);
+  }
+}
+
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  if (blockIdx.y == 0) get<DK>(k_out, k_pool, k_scale, table, held);
+  else get<DV>(v_out, v_pool, v_scale, table, held);
+}
+)KRN";
+
+// ------------------------------------------------------------------------------------------------ CacheAttention
+// For a query q of a head: o = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = q . k_j * scale * log2(e), over the keys j
+// that its sequence holds.  The keys are read once, for all query heads that share them; m may be any reference (see below).
+//
+// Four wavefronts, each with 32 keys per step.  S = K . Q^T by 16x16 MFMA: keys are the rows, the (up to 16) query heads of a
+// key head the columns, so that a lane holds eight scores of one query and the softmax needs two exchanges.  Those scores,
+// rounded, lie as the right operand of O^T = V^T . P^T needs them if the contraction takes the keys in the order
+// 4 h .. 4 h + 3, 16 + 4 h .. (h: a lane's quarter of the wavefront); the left operand, V transposed, is the same order of keys in
+// a lane's registers: every lane loads its channels of its eight keys and picks one channel of each.  Nothing but the final sums
+// goes through LDS.  Each wavefront has its own maximum and sums; they are joined at the end of a workgroup's keys, and a
+// second kernel joins the workgroups among which a sequence's keys were split.
+const char* kAttendBody = R"KRN(
+#define MASK_ALL 0xffffffffu
+#define SHARE (HQ / HEADS)
+#if POOL == 0
+#define KV 4
+#elif POOL == 1
+#define KV 8
+#else
+#define KV (DK % 64 == 0 ? 16 : 8)
+#endif
+#define NC ((DK + 4 * KV - 1) / (4 * KV))          // steps along a key's channels: four quarters of KV each
+typedef pool_t kvec_t __attribute__((ext_vector_type(KV)));
+
+// ---- operands of the two products
+#if POOL == 0
+typedef float qfrag_t;
+typedef float pfrag_t;
+#else
+typedef qelem_t qfrag_t __attribute__((ext_vector_type(8)));
+typedef pelem_t pfrag_t __attribute__((ext_vector_type(8)));
+#endif
+DEV qelem_t to_q(float v) { return (qelem_t)v; }
+
+// keys [begin, end) that sequence b attends over, the first step of this split and the step behind its last
+DEV void span_of(const int b, const int split, const int* __restrict__ held, int& begin, int& end, int& s0, int& s1, int& splits) {
+  end = min(max(held[b], 0), TABLE * SLOTS);
+  begin = WINDOW > 0 ? max(0, end - WINDOW) : 0;
+  const int tiles = (end + 31) / 32 - begin / 32, steps = end > begin ? (tiles + 3) / 4 : 0;
+  const int per = max(1, (steps + NSPLIT - 1) / NSPLIT);
+  splits = (steps + per - 1) / per;
+  s0 = min(split * per, steps);
+  s1 = min(s0 + per, steps);
+}
+
+template <int VW> struct vvec { typedef pool_t t __attribute__((ext_vector_type(VW))); };
+template <> struct vvec<1> { typedef pool_t t; };
+template <int VW> DEV pool_t pick(const typename vvec<VW>::t& v, int e) { if constexpr (VW == 1) return v; else return v[e]; }
+
+// O^T += V^T . P^T for the channels BASE + 16 VW of a lane's eight keys
+template <int BASE, int VW, int T0> DEV void values(f32x4* o, const pool_t* __restrict__ vp, const long long (&vrow)[8], const u32 seen, const pfrag_t (&p)[PN], const int n, const int h) {
+  typedef typename vvec<VW>::t vec_t;
+  vec_t x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = *(const vec_t*)(vp + vrow[j] * DV + BASE + n * VW);
+  // a masked key's probability is zero, but zero times what its slot happens to hold (an infinity, NaN) need not be
+  if (seen != MASK_ALL) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) x[j] = (vec_t)0;
+  }
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+#if POOL == 0
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[T0 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(pick<VW>(x[j], e), p[j], o[T0 + e], 0, 0, 0);
+#else
+    pfrag_t a;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) a[j] = POOL == 1 ? __builtin_bit_cast(pelem_t, (u16)pick<VW>(x[j], e)) : (pelem_t)(float)pick<VW>(x[j], e);
+#pragma unroll
+    for (int i = 0; i < PN; ++i) o[T0 + e] = PV_MFMA(a, p[i], o[T0 + e], 0, 0, 0);
+#endif
+  }
+}
+
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  __shared__ float Ms[4][16], Ls[4][16];
+  __shared__ __attribute__((aligned(16))) float Os[4][GQ][DV + 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
+  const int split = blockIdx.x % NSPLIT, rest = blockIdx.x / NSPLIT, q0 = rest % QTILES * 16, head = rest / QTILES % HEADS, b = rest / QTILES / HEADS;
+  int begin, end, s0, s1, splits;
+  span_of(b, split, held, begin, end, s0, s1, splits);
+  if (NSPLIT > 1 && s0 >= s1) return;
+  const int* __restrict__ row_of = table + (long long)b * TABLE;
+
+  // this lane's query (behind the last one: that again, computed and not stored)
+  const qin_t* __restrict__ qp = q + ((long long)b * HQ + head * SHARE + min(q0 + n, SHARE - 1)) * DK;
+#if POOL == 0
+  float rq[NC][4];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const f32x4 t = *(const f32x4*)(qp + c * 16 + h * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rq[c][e] = t[e];
+  }
+#else
+  qfrag_t rq[NC][KV / 8][QN];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int f = 0; f < KV / 8; ++f) {
+      const int d = (c * 4 + h) * KV + f * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = DK % (4 * KV) == 0 || d < DK ? cvt_in(qp[DK % (4 * KV) == 0 || d < DK ? d + e : 0]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < QN; ++i) { rq[c][f][i][e] = to_q(x); x -= (float)rq[c][f][i][e]; }
+      }
+    }
+#endif
+  f32x4 o[DV / 16];
+#pragma unroll
+  for (int t = 0; t < DV / 16; ++t) o[t] = 0.0f;
+  float m_run = -__builtin_inff(), l_run = 0.0f;
+
+  auto page_at = [&](const int step) {
+    const int lp = ((begin / 32 + step * 4 + wave) * 32 + (lane & 31)) / SLOTS;
+    return step < s1 && lp < TABLE ? row_of[lp] : -1;
+  };
+  int page_next = page_at(s0);
+  for (int step = s0; step < s1; ++step) {
+    const int k0 = (begin / 32 + step * 4 + wave) * 32, key = k0 + (lane & 31), page = page_next;
+    page_next = page_at(step + 1);
+    const bool there = (u32)page < (u32)PAGES;
+    const int row = there ? (page * HEADS + head) * SLOTS + key % SLOTS : 0;      // (a page that is not there: row 0, masked)
+    const u32 seen = (u32)__builtin_amdgcn_ballot_w64(there && key >= begin && key < end);
+    if (seen == 0) continue;
+
+    // ---- rows of this lane's keys: as a row of K, and as the eight keys of its scores
+    long long krow[2], vrow[8];
+    krow[0] = (u32)__shfl(row, n, 64);
+    krow[1] = (u32)__shfl(row, 16 + n, 64);
+#if SLOTS % 4 == 0
+    const long long g0 = (u32)__shfl(row, 4 * h, 64), g1 = (u32)__shfl(row, 16 + 4 * h, 64);      // (four consecutive keys share a page)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { vrow[j] = g0 + j; vrow[4 + j] = g1 + j; }
+#else
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vrow[j] = (u32)__shfl(row, j / 4 * 16 + 4 * h + j % 4, 64);
+#endif
+    kvec_t rk[2][NC];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int d = (c * 4 + h) * KV;
+        rk[u][c] = *(const kvec_t*)(k_pool + krow[u] * DK + (DK % (4 * KV) == 0 || d < DK ? d : 0));
+        if (DK % (4 * KV) != 0 && d >= DK) rk[u][c] = 0;
+      }
+#if POOL == 2
+    float ks[8], vs[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { ks[j] = k_scale[vrow[j]]; vs[j] = v_scale[vrow[j]]; }
+#endif
+    // ---- scores: element i of tile u is key 16 u + 4 h + i of query n
+    float s[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 acc = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+#if POOL == 0
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(rk[u][c][e], rq[c][e], acc, 0, 0, 0);
+#else
+#pragma unroll
+        for (int f = 0; f < KV / 8; ++f) {
+          qfrag_t a;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = POOL == 1 ? __builtin_bit_cast(qelem_t, (u16)rk[u][c][f * 8 + e]) : to_q((float)rk[u][c][f * 8 + e]);
+#pragma unroll
+          for (int i = 0; i < QN; ++i) acc = QK_MFMA(a, rq[c][f][i], acc, 0, 0, 0);
+        }
+#endif
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[u * 4 + i] = acc[i] * SCALE;
+    }
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+#if POOL == 2
+      s[j] *= ks[j];
+#endif
+      if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) s[j] = -__builtin_inff();
+      mx = fmaxf(mx, s[j]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    // The reference of the exponentials moves only when a row's maximum has grown by more than 2^8: until then the
+    // probabilities reach at most 256, harmless in fp32 sums and in the operand, and nothing has to be rescaled.
+    const float cand = fmaxf(m_run, mx);
+    const bool move = cand - m_run > 8.0f;                       // (also for the first finite maximum, m_run = -inf)
+    if (__builtin_amdgcn_ballot_w64(move) != 0) {
+      const float m_next = move ? cand : m_run;
+      const float alpha = m_next == m_run ? 1.0f : dn_exp2(m_run - m_next);
+      m_run = m_next;
+      l_run *= alpha;
+#pragma unroll
+      for (int t = 0; t < DV / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][i] *= alpha;
+    }
+    const float m2 = m_run == -__builtin_inff() ? 0.0f : m_run;
+    pfrag_t p[PN];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float x = dn_exp2(s[j] - m2);
+      l_run += x;                                                // the sum keeps fp32
+#if POOL == 2
+      x = seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? x * vs[j] : 0.0f;
+#endif
+#if POOL == 0
+      p[j] = x;
+#else
+#pragma unroll
+      for (int i = 0; i < PN; ++i) { p[i][j] = (pelem_t)x; x -= (float)p[i][j]; }
+#endif
+    }
+    VALUES
+  }
+
+  // ---- the workgroup's four wavefronts joined
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (h == 0) { Ms[wave][n] = m_run; Ls[wave][n] = l_run; }
+  if (n < GQ) {
+    OUT_TO_LDS
+  }
+  __syncthreads();
+  for (int i = tid; i < GQ * DV; i += 256) {
+    const int r = i / DV, d = i % DV;
+    if (q0 + r >= SHARE) break;
+    const float m = fmaxf(fmaxf(Ms[0][r], Ms[1][r]), fmaxf(Ms[2][r], Ms[3][r]));
+    float l = 0.0f, x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float a = m == -__builtin_inff() ? 0.0f : dn_exp2(Ms[w][r] - m);
+      l += a * Ls[w][r];
+      x += a * Os[w][r][d];
+    }
+    const long long at = (long long)b * HQ + head * SHARE + q0 + r;
+#if NSPLIT > 1
+    scratch[PART_AT + (at * NSPLIT + split) * DV + d] = x;
+    if (d == 0) { scratch[(at * NSPLIT + split) * 2] = m; scratch[(at * NSPLIT + split) * 2 + 1] = l; }
+#else
+    qin_t y;
+    cvt_out(&y, l == 0.0f ? 0.0f : x / l);                      // (no key, or all of them at -infinity: zeros)
+    out[at * DV + d] = y;
+#endif
+  }
+}
+)KRN";
+
+// Joins the splits of one query: weights 2^(m_s - m) / l, l = sum_s 2^(m_s - m) l_s; a workgroup's threads are DV channels wide and
+// share the splits among the rest.
+const char* kJoinBody = R"KRN(
+#define ROWS (256 / DV > 0 ? 256 / DV : 1)
+DEV void span_of(const int b, const int* __restrict__ held, int& splits) {
+  const int end = min(max(held[b], 0), TABLE * SLOTS), begin = WINDOW > 0 ? max(0, end - WINDOW) : 0;
+  const int tiles = (end + 31) / 32 - begin / 32, steps = end > begin ? (tiles + 3) / 4 : 0;
+  const int per = max(1, (steps + NSPLIT - 1) / NSPLIT);
+  splits = (steps + per - 1) / per;
+}
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  __shared__ float w[NSPLIT], part[ROWS][DV];
+  const int tid = threadIdx.x;
+  const long long at = blockIdx.x;
+  int splits;
+  span_of((int)(at / HQ), held, splits);
+  const float* __restrict__ ml = scratch + at * NSPLIT * 2;
+  if (tid < 64) {
+    float m = -__builtin_inff();
+    for (int s = tid; s < splits; s += 64) m = fmaxf(m, ml[s * 2]);
+    m = dn_wave_max(m);
+    float l = 0.0f;
+    for (int s = tid; s < splits; s += 64) {
+      const float a = m == -__builtin_inff() ? 0.0f : dn_exp2(ml[s * 2] - m);
+      w[s] = a;
+      l += a * ml[s * 2 + 1];
+    }
+    l = dn_wave_sum(l);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    for (int s = tid; s < splits; s += 64) w[s] = inv == 0.0f && l == 0.0f ? 0.0f : w[s] * inv;
+  }
+  __syncthreads();
+  const int d = tid % DV, r = tid / DV;
+  if (r < ROWS) {
+    float x = 0.0f;
+    const float* __restrict__ p = scratch + PART_AT + at * NSPLIT * DV + d;
+    for (int s = r; s < splits; s += ROWS) x += w[s] * p[(long long)s * DV];
+    part[r][d] = x;
+  }
+  __syncthreads();
+  if (tid < DV) {
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) x += part[i][tid];
+    qin_t y;
+    cvt_out(&y, x);
+    out[at * DV + tid] = y;
+  }
+}
+)KRN";
+
+Launch make_launch(const std::string& prefix, const std::string& head, const char* body, std::vector<int> params, int64_t blocks) {
+  DNNF_CHECK(blocks >= 1 && blocks < (int64_t)1 << 31, DNNF_UNSUPPORTED_OP, "cache operator: more workgroups than one launch takes");
+  Launch L;
+  std::string src = std::string(device_preamble()) + head + body;
+  L.name = fnv_name(prefix, src);
+  size_t pos;
+  while ((pos = src.find("KNAME")) != std::string::npos) src.replace(pos, 5, L.name);
+  L.source = src;
+  L.params = std::move(params);
+  L.grid[0] = (unsigned)blocks;
+  L.block[0] = 256;
+  return L;
+}
+
+}  // namespace
+
+Lowered lower_cache(LowerCtx& c) {
+  const Graph& g = c.g;
+  DNNF_CHECK(c.blk.ops.size() == 1, DNNF_UNSUPPORTED_OP, "a cache operator is a block of its own");
+  const Op& op = g.ops[c.blk.ops[0]];
+  check_decode_op(g, op);
+  const CacheOperands o = cache_operands(g, op);
+  const OpClass cls = op.info->cls;
+  // (16-bit rows that are attended over go to the matrix units as they are: plain bits)
+  const int stored = g.tensors[o.pool[0]].dtype;
+  const std::string pool = o.eight_bits ? "signed char" : cls == OC_CACHE_ATTN && dtype_bytes(stored) == 2 ? "u16" : c.ctype(stored);
+  Lowered L;
+  L.family = FAM_CACHE;
+  L.ext_in = op.in;
+  L.ext_out = op.out;
+  std::ostringstream k;
+  k << "typedef " << pool << " pool_t;\n#define EIGHT_BITS " << (int)o.eight_bits << "\n#define PAGES " << o.P << "\n#define HEADS " << o.HK << "\n#define SLOTS "
+    << o.S << "\n#define DK " << o.D[0] << "\n#define DV " << o.D[1] << "\n#define SEQUENCES " << o.B << "\n#define TABLE " << o.M << "\n";
+  auto scales = [&](bool written) {      // the parameters of the scales, or what stands for them in a pool without
+    const std::string cst = written ? "" : "const ";
+    return o.eight_bits ? ", " + cst + "float* __restrict__ k_scale, " + cst + "float* __restrict__ v_scale" : std::string();
+  };
+  if (!o.eight_bits) k << "#define k_scale ((float*)0)\n#define v_scale ((float*)0)\n";
+  std::vector<int> params;
+
+  if (cls == OC_CACHE_WRITE) {
+    const std::string elem = c.ctype(g.tensors[o.fresh[0]].dtype);
+    const int64_t vec = 16 / dtype_bytes(g.tensors[o.fresh[0]].dtype), chunk = std::min<int64_t>(o.S, 16);
+    const int64_t spans = (o.T + o.S - 2) / o.S + 1, subs = (o.S + chunk - 1) / chunk;
+    int64_t lanes = 1;
+    while (lanes * vec < std::max(o.D[0], o.D[1])) lanes *= 2;
+    DNNF_CHECK(o.B * spans < (int64_t)1 << 30, DNNF_UNSUPPORTED_OP, "CacheWrite: too many pages in one call");
+    k << "typedef " << elem << " elem_t;\n#define TOKENS " << o.T << "\n#define SPANS " << spans << "\n#define SUBS " << subs << "\n#define CHUNK " << chunk
+      << "\n#define LANES " << lanes << "\n#define HAS_COUNT " << (int)(o.count >= 0) << "\n";
+    if (o.count < 0) k << "#define count ((const int*)0)\n";
+    k << "#define KPARAMS pool_t* __restrict__ k_pool, pool_t* __restrict__ v_pool" << scales(true) << ", const elem_t* __restrict__ k, const elem_t* __restrict__ v, "
+      << "const int* __restrict__ table, const int* __restrict__ first" << (o.count >= 0 ? ", const int* __restrict__ count" : "") << "\n";
+    params = op.out;
+    for (int t : {o.fresh[0], o.fresh[1], o.table, o.first}) params.push_back(t);
+    if (o.count >= 0) params.push_back(o.count);
+    for (size_t i = 0; i < op.out.size(); i++) L.in_place.push_back({op.out[i], op.in[i]});
+    L.launches.push_back(make_launch("dnnf_cache_write", k.str(), kWriteBody, params, o.B * spans * subs));
+    L.variant = "cache_write_chunk" + std::to_string(chunk) + (o.eight_bits ? "_i8" : "");
+    return L;
+  }
+
+  params = {o.pool[0], o.pool[1]};
+  if (o.eight_bits) { params.push_back(o.scale[0]); params.push_back(o.scale[1]); }
+  params.push_back(o.table);
+  params.push_back(o.held);
+  const std::string pools = "const pool_t* __restrict__ k_pool, const pool_t* __restrict__ v_pool" + scales(false) + ", const int* __restrict__ table, const int* __restrict__ held";
+  if (cls == OC_CACHE_READ) {
+    const int dt = g.tensors[op.out[0]].dtype;
+    const int64_t vec = 16 / dtype_bytes(dt), most = o.B * o.T * o.HK * (std::max(o.D[0], o.D[1]) / vec);
+    k << "typedef " << c.ctype(dt) << " elem_t;\ntypedef " << (most < ((int64_t)1 << 31) - 1024 ? "int" : "long long") << " idx_t;\n#define LENGTH " << o.T << "\n";
+    k << "#define KPARAMS " << pools << ", elem_t* __restrict__ k_out, elem_t* __restrict__ v_out\n";
+    params.push_back(op.out[0]);
+    params.push_back(op.out[1]);
+    L.launches.push_back(make_launch("dnnf_cache_read", k.str(), kReadBody, params, (most + 1023) / 1024));
+    L.launches[0].grid[1] = 2;
+    L.variant = std::string("cache_read") + (o.eight_bits ? "_i8" : "");
+    return L;
+  }
+
+  // ---- attention
+  const int dt = g.tensors[o.q].dtype;
+  const int64_t share = o.HQ / o.HK, qtiles = (share + 15) / 16;
+  const int64_t window = op.i("window", 0), most = window > 0 ? std::min(window + 31, o.M * o.S) : o.M * o.S;
+  const double scale = op.has("scale") ? op.f("scale", 1) : 1.0 / std::sqrt((double)o.D[0]);
+  // Workgroups for about four per compute unit, and at least one step (128 keys) each at the table's capacity.  Behind
+  // shorter sequences the splits a kernel does not need end at once.
+  const int64_t units = o.B * o.HK * qtiles, steps = (most + 127) / 128;
+  const int64_t nsplit = std::max<int64_t>(1, std::min<int64_t>({steps, (1024 + units - 1) / units, 128}));
+  const int form = o.eight_bits ? 2 : dt == DNNF_F32 ? 0 : 1;
+  char num[40];
+  snprintf(num, sizeof num, "%.9gf", scale * 1.4426950408889634);
+  std::string sc = num;
+  if (sc.find_first_of(".e") == std::string::npos) sc.insert(sc.size() - 1, ".0");
+  const int64_t rows = o.B * o.HQ, part_at = (rows * nsplit * 2 + 3) / 4 * 4;
+  k << "typedef " << c.ctype(dt) << " qin_t;\n#define POOL " << form << "\n#define HQ " << o.HQ << "\n#define WINDOW " << window << "\n#define NSPLIT " << nsplit
+    << "\n#define QTILES " << qtiles << "\n#define GQ " << std::min<int64_t>(share, 16) << "\n#define SCALE " << sc << "\n#define PART_AT " << part_at << "\n";
+  // Types of the products' operands.  Pools of 16 bits: queries and rows as they are.  Pools of 8 bits: rows are whole numbers up
+  // to 127, exact in either type; a value's step goes to its probability, whose range only bfloat16 has.  Probabilities are
+  // given in two parts (three for fp32 results): rounded once to 8 bits they would add as much error as the rounding of the
+  // result (1.4 times its error in all), and the matrix units have time for the second part.
+  const std::string h16 = dt == DNNF_F16 ? "_Float16" : "__bf16", mf = "__builtin_amdgcn_mfma_f32_16x16x32_";
+  const int qn = form == 2 && dt == DNNF_F32 ? 3 : 1, pn = form == 0 ? 8 : dt == DNNF_F32 ? 3 : 2;
+  k << "typedef " << (form == 0 ? "float" : h16) << " qelem_t;\ntypedef " << (form == 0 ? "float" : form == 1 ? h16 : "__bf16") << " pelem_t;\n#define QN " << qn << "\n#define PN " << pn
+    << "\n#define QK_MFMA " << mf << (dt == DNNF_F16 ? "f16" : "bf16") << "\n#define PV_MFMA " << mf << (form == 1 && dt == DNNF_F16 ? "f16" : "bf16") << "\n";
+  // a value's channels in runs of 128, 64, 32 and 16: 8, 4, 2 or 1 for each of the sixteen lanes of a quarter (fp32: 64 at most,
+  // 16-byte loads)
+  std::string values, to_lds;
+  int tile = 0;
+  for (int64_t at = 0; at < o.D[1];) {
+    int64_t w = form == 0 ? 4 : 8;
+    while (w * 16 > o.D[1] - at) w /= 2;
+    values += "    values<" + std::to_string(at) + ", " + std::to_string(w) + ", " + std::to_string(tile) + ">(o, v_pool, vrow, seen, p, n, h); \\\n";
+    for (int64_t e = 0; e < w; e++)
+      for (int i = 0; i < 4; i++)
+        to_lds += "    Os[wave][n][" + std::to_string(at + e + i * w) + " + h * " + std::to_string(4 * w) + "] = o[" + std::to_string(tile + e) + "][" + std::to_string(i) + "]; \\\n";
+    tile += (int)w;
+    at += 16 * w;
+  }
+  const std::string head = k.str();
+  params.insert(params.begin(), o.q);
+  if (nsplit == 1) params.push_back(op.out[0]);
+  const std::string main_params = "#define KPARAMS const qin_t* __restrict__ q, " + pools + (nsplit > 1 ? ", float* __restrict__ scratch" : ", qin_t* __restrict__ out") + "\n";
+  L.launches.push_back(make_launch("dnnf_cache_attend", head + main_params + "#define VALUES \\\n" + values + "\n#define OUT_TO_LDS \\\n" + to_lds + "\n", kAttendBody, params, units * nsplit));
+  if (nsplit > 1) {
+    L.launches[0].scratch = true;
+    L.scratch_bytes = (part_at + rows * nsplit * o.D[1]) * 4;
+    L.launches.push_back(make_launch("dnnf_cache_join", head + "#define KPARAMS const int* __restrict__ held, qin_t* __restrict__ out, const float* __restrict__ scratch\n",
+                                     kJoinBody, {o.held, op.out[0]}, rows));
+    L.launches[1].scratch = true;
+  }
+  L.variant = "cache_attend_split" + std::to_string(nsplit) + (form == 2 ? "_i8" : form == 0 ? "_f32" : "_16");
+  return L;
+}
+
+}  // namespace dnnf

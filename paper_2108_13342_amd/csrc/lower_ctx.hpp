@@ -169,6 +169,8 @@ Lowered lower_conv3d(LowerCtx& c);
 Lowered lower_conv_transpose(LowerCtx& c);
 Lowered lower_pool(LowerCtx& c);
 Lowered lower_scan(LowerCtx& c);
+Lowered lower_cache(LowerCtx& c);        // CacheWrite, CacheRead, CacheAttention: each a block of its own
+Lowered lower_int4(LowerCtx& c);         // MatMulInt4 (+ successors)
 // MatMul -> One-to-One operators -> Softmax -> MatMul (+ successors) as one streaming-softmax kernel
 Lowered lower_attention(const Graph& g, const Block& b, const LowerOpts& o);
 

@@ -1,0 +1,331 @@
+// Products with weights of four bits: y[m, n] = sum_k x[m, k] * (code[n, k] - zero[n, k / G]) * scale[n, k / G], for the few rows of
+// single-token inference.  The block may hold One-to-One operators, Reshapes and Splits behind the product, as behind MatMul.
+//
+// What bounds it: the weights, half a byte each and read once; everything else has to stay out of their way.
+//   - A code becomes an operand of the matrix units by two instructions for two codes: shifted into the mantissa of 16 it is the
+//     number 16 + code, exactly, in float16 and bfloat16 alike.  The product of a group is then taken as
+//     sum x (16 + code) - (16 + zero) sum x; the row sums of x come from the matrix units too (a column of ones), in the layout
+//     that the results have, so that a group costs two fp32 instructions per result.  (Infinite or NaN x: the row is NaN.)
+//   - The order of k within a contraction step is free as long as both operands have the same: a lane takes the codes in the order
+//     in which they leave a 32-bit word (0, 4, 1, 5, 2, 6, 3, 7), and x is picked in that order.
+//   - A wavefront reads 16 weight rows, 16 bytes a lane: 128 codes a row.  In groups of 128 and more a lane's 32 codes go into
+//     four steps as they are (each step meets all four quarters of the run).  Smaller groups have to meet 32 successive codes in a step:
+//     four exchanges between the wavefront's quarters turn the 4 x 4 words around.
+//   - fp32 x is taken in three bfloat16 parts, which hold all of its 24 bits; weights are exact in either case.
+// The wavefronts of a workgroup share its columns and split K among them; sums are joined in LDS in a fixed order.
+#include <algorithm>
+#include <sstream>
+
+#include "lower_ctx.hpp"
+
+namespace dnnf {
+
+namespace {
+
+const char* kInt4Body = R"KRN(
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef elem_t xvec_t __attribute__((ext_vector_type(8), aligned(ELEM_BYTES)));
+typedef part_t frag_t __attribute__((ext_vector_type(8)));
+#define CHUNK 128                                  // codes of a row that a wavefront reads at once
+#define CHUNKS ((GK + CHUNK - 1) / CHUNK)
+#define ROW_BYTES ((GK + 1) / 2)
+#define PARTS_OF_CHUNK (4 / STEPS)                 // groups, or pieces of one, in a chunk
+#define ROWS (GM < 16 * MT ? GM : 16 * MT)
+
+struct run_t {
+  u32x4 w[NT];
+  elem_t s[NT][PARTS_OF_CHUNK];
+  unsigned char z[NT][PARTS_OF_CHUNK];
+};
+
+// x[row, k .. k + 8) in the order of a word's codes, in XP parts
+DEV void load_x(const elem_t* __restrict__ xr, const int k, frag_t (&f)[XP]) {
+  float v[8];
+  elem_t e[8];
+  if (GK % 8 == 0 ? (GK % CHUNK == 0 || k < GK) : k + 8 <= GK) {
+    const xvec_t t = *(const xvec_t*)(xr + k);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = t[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { e[j] = 0; if (k + j < GK) e[j] = xr[k + j]; }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int slot = j < 4 ? 2 * j : 2 * (j - 4) + 1;
+#if XP == 1
+    f[0][slot] = __builtin_bit_cast(part_t, e[j]);
+#else
+    v[j] = e[j];
+#pragma unroll
+    for (int i = 0; i < XP; ++i) { f[i][slot] = (part_t)v[j]; v[j] -= (float)f[i][slot]; }
+#endif
+  }
+}
+
+// eight codes of a word as 16 + code
+DEV frag_t decode(const u32 w) {
+  u32x4 r;
+#if F16_PARTS
+  r[0] = (w << 6 & 0x03c003c0u) | 0x4c004c00u;
+  r[1] = (w << 2 & 0x03c003c0u) | 0x4c004c00u;
+  r[2] = (w >> 2 & 0x03c003c0u) | 0x4c004c00u;
+  r[3] = (w >> 6 & 0x03c003c0u) | 0x4c004c00u;
+#else
+  r[0] = (w << 3 & 0x00780078u) | 0x41804180u;
+  r[1] = (w >> 1 & 0x00780078u) | 0x41804180u;
+  r[2] = (w >> 5 & 0x00780078u) | 0x41804180u;
+  r[3] = (w >> 9 & 0x00780078u) | 0x41804180u;
+#endif
+  return __builtin_bit_cast(frag_t, r);
+}
+
+extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
+  __shared__ __attribute__((aligned(16))) float part[WAVES][ROWS][16 * NT + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
+  const idx_t c0 = (idx_t)blockIdx.x * (16 * NT), r0 = (idx_t)blockIdx.y * (16 * MT);
+  const unsigned char* __restrict__ wr[NT];
+  const elem_t* __restrict__ sr[NT];
+  const unsigned char* __restrict__ zr[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const idx_t col = min(c0 + t * 16 + n, (idx_t)(GN - 1));         // (behind the last column: that again, not stored)
+    wr[t] = PW + (long long)col * ROW_BYTES;
+    sr[t] = PS + (long long)col * GROUPS;
+#if HAS_ZERO
+    zr[t] = PZ + (long long)col * GROUPS;
+#endif
+  }
+  const elem_t* __restrict__ xr[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) xr[t] = PX + offX_batch(0) + offX_row(min(r0 + t * 16 + n, (idx_t)(GM - 1)));
+
+  auto load = [&](run_t& r, const int c) {
+    if (c >= CHUNKS) return;
+    const int at = c * (CHUNK / 2) + h * 16;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (ROW_BYTES % 64 == 0 || at + 16 <= ROW_BYTES) r.w[t] = *(const u32x4_any*)(wr[t] + at);
+      else {
+        // the end of a row (codes behind it are multiplied by zeros)
+        r.w[t] = 0;
+        if (ROW_BYTES % 16 != 0) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (at + i < ROW_BYTES) r.w[t][i / 4] |= (u32)wr[t][at + i] << (i % 4 * 8);
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < PARTS_OF_CHUNK; ++p) {
+        const int g = min((c * CHUNK + p * STEPS * 32) / GROUP, GROUPS - 1);
+        r.s[t][p] = sr[t][g];
+#if HAS_ZERO
+        r.z[t][p] = zr[t][g];
+#endif
+      }
+    }
+  };
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int u = 0; u < NT; ++u) acc[t][u] = 0.0f;
+  frag_t ones;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) ones[j] = (part_t)1.0f;
+
+  auto multiply = [&](run_t& r, const int c) {
+#if STEPS < 4
+    // words (quarter q, register i) -> (quarter i, register q)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const u32x2 a = __builtin_amdgcn_permlane32_swap(r.w[t][0], r.w[t][2], false, false), b = __builtin_amdgcn_permlane32_swap(r.w[t][1], r.w[t][3], false, false);
+      const u32x2 p = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), q = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+      r.w[t] = (u32x4){p[0], p[1], q[0], q[1]};
+    }
+#endif
+#pragma unroll
+    for (int p = 0; p < PARTS_OF_CHUNK; ++p) {
+      f32x4 sum[MT][NT], sx[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        sx[t] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) sum[t][u] = 0.0f;
+      }
+#pragma unroll
+      for (int i = p * STEPS; i < (p + 1) * STEPS; ++i) {
+        const int k = c * CHUNK + (STEPS == 4 ? h * 32 + i * 8 : i * 32 + h * 8);
+        frag_t w[NT];
+#pragma unroll
+        for (int u = 0; u < NT; ++u) w[u] = decode(r.w[u][i]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          frag_t x[XP];
+          load_x(xr[t], k, x);
+#pragma unroll
+          for (int q = 0; q < XP; ++q) {
+            sx[t] = MFMA(x[q], ones, sx[t], 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < NT; ++u) sum[t][u] = MFMA(x[q], w[u], sum[t][u], 0, 0, 0);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        const float s = cvt_in(r.s[u][p]), z = HAS_ZERO ? 16.0f + (float)r.z[u][p] : 24.0f;
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[t][e], sum[t][u][e]), acc[t][u][e]);
+      }
+    }
+  };
+
+  run_t ring[AHEAD];
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p) load(ring[p], wave + p * WAVES);
+  for (int c = wave; c < CHUNKS; c += WAVES * AHEAD) {
+#pragma unroll
+    for (int p = 0; p < AHEAD; ++p) {
+      const int cc = c + p * WAVES;
+      if (cc >= CHUNKS) break;
+      multiply(ring[p], cc);
+      load(ring[p], cc + WAVES * AHEAD);
+    }
+  }
+
+  // ---- the wavefronts' sums, joined; result (4 h + e, n) of a 16x16 tile is element e
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (t * 16 + 4 * h + e < ROWS) part[wave][t * 16 + 4 * h + e][u * 16 + n] = acc[t][u][e];
+  __syncthreads();
+  for (int i = tid; i < ROWS * 16 * NT; i += 64 * WAVES) {
+    const int rl = i / (16 * NT), cl = i % (16 * NT);
+    if (r0 + rl >= GM || c0 + cl >= GN) continue;
+    float v = part[0][rl][cl];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += part[w][rl][cl];
+    float cv[NCOLV > 0 ? NCOLV : 1];
+    col_loads(c0 + cl, cv, KARGS);
+    epilogue(0, r0 + rl, c0 + cl, v, cv, KARGS);
+  }
+}
+)KRN";
+
+}  // namespace
+
+Lowered lower_int4(LowerCtx& c) {
+  const Graph& g = c.g;
+  const Op& A = g.ops[c.anchor_op];
+  check_decode_op(g, A);
+  const Tensor &X = g.tensors[A.in[0]], &C = g.tensors[A.out[0]];
+  const int64_t K = X.dims.back(), N = C.dims.back(), M = C.n() / N, G = A.i("group_size", 0), groups = (K + G - 1) / G;
+  const bool has_zero = A.in.size() == 4;
+
+  // ---- index space: the result's axes and the contraction
+  TIdx oi = c.fresh_index(C.dims);
+  const int katom = c.new_atom(K);
+  TIdx xi = oi;
+  xi.back() = DimIdx();
+  if (K > 1) xi.back().atoms = {katom};
+  c.tidx[c.anchor_out] = oi;
+  std::vector<int> ein, eout, removed;
+  block_io(g, c.blk, ein, eout, removed);
+  c.forward_all();
+  for (int t : eout) DNNF_CHECK(c.tidx.count(t), DNNF_UNSUPPORTED_OP, "block output " + g.tensors[t].name + " does not follow the contraction");
+  c.collect_stores(eout);
+  const int xn = c.value(A.in[0], xi);
+  DNNF_CHECK(c.nodes[xn].kind == ENode::LOAD && c.nodes[xn].addr.indirect.empty() && g.tensors[c.nodes[xn].tensor].dtype == X.dtype, DNNF_UNSUPPORTED_OP,
+             "arithmetic in front of a product with 4-bit weights has no kernel template");
+  const int tx = c.nodes[xn].tensor;
+  const Affine xa = c.resolved(c.nodes[xn].addr);
+  std::vector<int> katoms, cols, rows;
+  c.resolve({katom}, katoms);
+  DNNF_CHECK(katoms.size() <= 1 && (katoms.empty() || stride_of(xa, katoms[0]) == 1), DNNF_UNSUPPORTED_OP, "x is not contiguous along the contraction");
+  c.resolve(oi.back().atoms, cols);
+  for (size_t d = 0; d + 1 < oi.size(); d++) c.resolve(oi[d].atoms, rows);
+  DNNF_CHECK(c.extent_of(rows) == M && c.extent_of(cols) == N, DNNF_UNSUPPORTED_OP, "axes of a product with 4-bit weights");
+
+  // ---- parameters
+  std::vector<int> params = {tx, A.in[1], A.in[2]};
+  if (has_zero) params.push_back(A.in[3]);
+  std::map<int, int> pslot;
+  std::set<int> written;
+  {
+    std::set<int> seen;
+    std::vector<int> stack;
+    for (auto& s : c.stores) stack.push_back(s.value);
+    while (!stack.empty()) {
+      const int n = stack.back();
+      stack.pop_back();
+      if (!seen.insert(n).second) continue;
+      for (int a : c.nodes[n].args) stack.push_back(a);
+      if (c.nodes[n].kind == ENode::LOAD) {
+        DNNF_CHECK(c.nodes[n].addr.indirect.empty(), DNNF_UNSUPPORTED_OP, "gathered operand behind a product with 4-bit weights");
+        if (!pslot.count(c.nodes[n].tensor)) { pslot[c.nodes[n].tensor] = (int)params.size(); params.push_back(c.nodes[n].tensor); }
+      }
+    }
+  }
+  const size_t n_in = params.size();
+  for (auto& s : c.stores) {
+    DNNF_CHECK(!pslot.count(s.tensor) && std::find(params.begin(), params.begin() + n_in, s.tensor) == params.begin() + n_in, DNNF_UNSUPPORTED_OP,
+               "block reads and writes the same tensor");
+    pslot[s.tensor] = (int)params.size();
+    params.push_back(s.tensor);
+    written.insert(s.tensor);
+  }
+  bool wide = false;
+  for (int t : params) wide = wide || g.tensors[t].n() >= (int64_t)1 << 31;
+  wide = wide || M * N >= (int64_t)1 << 31;
+
+  // ---- tile: all rows up to 64; as many columns as leave two workgroups per compute unit; K split among the wavefronts
+  const int64_t MT = std::min<int64_t>(4, (M + 15) / 16), row_tiles = (M + 16 * MT - 1) / (16 * MT), chunks = (K + 127) / 128;
+  int64_t NT = 4;
+  while (NT > 1 && (N + 16 * NT - 1) / (16 * NT) * row_tiles < 512) NT /= 2;
+  const int64_t waves = std::min<int64_t>(8, chunks), ahead = std::min<int64_t>(2, (chunks + waves - 1) / waves);
+  const int steps = G % 128 == 0 || G >= K ? 4 : G % 64 == 0 ? 2 : 1;
+
+  std::ostringstream k;
+  const std::string part = X.dtype == DNNF_F16 ? "_Float16" : "__bf16";
+  k << "typedef " << (wide ? "long long" : "int") << " idx_t;\ntypedef " << c.ctype(X.dtype) << " elem_t;\ntypedef " << part << " part_t;\n";
+  k << "#define ELEM_BYTES " << dtype_bytes(X.dtype) << "\n#define XP " << (X.dtype == DNNF_F32 ? 3 : 1) << "\n#define F16_PARTS " << (int)(X.dtype == DNNF_F16) << "\n";
+  k << "#define MFMA __builtin_amdgcn_mfma_f32_16x16x32_" << (X.dtype == DNNF_F16 ? "f16" : "bf16") << "\n";
+  k << "#define GM " << M << "\n#define GN " << N << "\n#define GK " << K << "\n#define GROUP " << G << "\n#define GROUPS " << groups << "\n#define HAS_ZERO " << (int)has_zero << "\n";
+  k << "#define MT " << MT << "\n#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define STEPS " << steps << "\n";
+  k << "#define PX p0\n#define PW p1\n#define PS p2\n#define PZ p3\n";
+  k << gemm_offset_fn(c, "offX_row", rows, xa) << gemm_offset_fn(c, "offX_batch", {}, xa);
+  const std::string kparams = c.param_list(params, written);
+  std::string kargs;
+  for (size_t i = 0; i < params.size(); i++) kargs += (i ? ", p" : "p") + std::to_string(i);
+  k << gemm_epilogue_source(c, {}, rows, cols, pslot, kparams, N, -1);
+  k << "#define KPARAMS " << kparams << "\n#define KARGS " << kargs << "\n" << kInt4Body;
+
+  Lowered L;
+  L.family = FAM_INT4;
+  L.ext_in.assign(params.begin(), params.begin() + n_in);
+  L.ext_out.assign(params.begin() + n_in, params.end());
+  Launch Kn;
+  Kn.params = params;
+  Kn.grid[0] = (unsigned)((N + 16 * NT - 1) / (16 * NT));
+  DNNF_CHECK(row_tiles < 65536, DNNF_UNSUPPORTED_OP, "MatMulInt4: too many rows for one launch");
+  Kn.grid[1] = (unsigned)row_tiles;
+  Kn.block[0] = (unsigned)(64 * waves);
+  std::string src = std::string(device_preamble()) + k.str();
+  Kn.name = fnv_name("dnnf_int4", src);
+  size_t pos;
+  while ((pos = src.find("KNAME")) != std::string::npos) src.replace(pos, 5, Kn.name);
+  Kn.source = src;
+  L.launches.push_back(Kn);
+  L.variant = "int4_" + std::to_string(16 * MT) + "x" + std::to_string(16 * NT) + "_w" + std::to_string(waves) + "_g" + std::to_string(32 * steps);
+  return L;
+}
+
+}  // namespace dnnf

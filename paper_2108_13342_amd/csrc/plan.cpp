@@ -196,6 +196,9 @@ void Plan::layout_workspace() {
     for (int t : pb.low.ext_out)
       if (g.tensors[t].kind == DNNF_INTERMEDIATE) place(t);
   }
+  // results that are an operand's storage, updated (CacheWrite)
+  for (auto& pb : blocks)
+    for (auto& pr : pb.low.in_place) alias_of[pr.first] = pr.second;
   // stacking Concats: the operands live inside the result (build_plan has made sure no tensor is claimed twice)
   for (auto& pb : blocks)
     if (pb.low.family == FAM_ALIAS && !pb.low.alias_parts.empty())
@@ -231,6 +234,13 @@ void* Plan::resolve(int t, const void* const* in, void* const* out, void* ws) co
 void Plan::launch_block(size_t b, const void* const* in, void* const* out, void* ws, void* stream) {
   PlanBlock& pb = blocks[b];
   DNNF_CHECK(pb.low.family >= 0, DNNF_UNSUPPORTED_OP, "block has no kernel (plan was built for analysis only): " + pb.low.variant);
+  for (size_t i = 0; i < pb.low.in_place.size(); i++) {
+    const Tensor &R = g.tensors[pb.low.in_place[i].first], &X = g.tensors[pb.low.in_place[i].second];
+    const void* at = resolve(pb.low.in_place[i].second, in, out, ws);
+    DNNF_CHECK(out && out[R.ext_index] == at, DNNF_INVALID_ARG, "output " + R.name + " is input " + X.name + " updated in place: both take the same pointer");
+    for (size_t j = 0; j < i; j++)
+      DNNF_CHECK(resolve(pb.low.in_place[j].second, in, out, ws) != at, DNNF_INVALID_ARG, "two tensors that are updated in place share one buffer: " + X.name);
+  }
   for (size_t li = 0; li < pb.low.launches.size(); li++) {
     const Launch& L = pb.low.launches[li];
     if (pb.fn.size() <= li) pb.fn.resize(pb.low.launches.size(), nullptr);

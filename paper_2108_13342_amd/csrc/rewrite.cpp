@@ -133,6 +133,10 @@ struct Rewriter {
       const Tensor& I = g.tensors[in];
       const Tensor& O = g.tensors[out];
       if (!is_float(I.dtype) || !is_float(O.dtype)) continue;
+      // (the cache operators and MatMulInt4 read and write tensors of the types their operands fix together)
+      bool typed = producer(in) && is_decode_op(*producer(in));
+      for (int c : O.consumers) typed = typed || is_decode_op(g.ops[c]);
+      if (typed) continue;
       const bool widening = I.dtype == O.dtype || (dtype_bytes(O.dtype) > dtype_bytes(I.dtype));
       if (widening && O.kind != DNNF_OUTPUT) {
         replace_uses(out, in);

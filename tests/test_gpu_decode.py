@@ -1,0 +1,419 @@
+"""The operators of single-token inference against their definitions in 64 bits: a paged key / value cache written in place,
+read back and attended over, and products with weights of four bits."""
+import numpy as np
+import pytest
+
+import decode_graphs as dg
+from oracle.interp import run_graph
+
+pytestmark = pytest.mark.gpu
+
+
+def run(spec, **kw):
+    from paper_2108_13342_amd import api
+
+    s = api.Session(spec, guard_bytes=256, **kw)
+    s.run()
+    got = s.result()
+    assert s.guards_intact(), f"{spec.name}: a kernel wrote outside an output buffer or the workspace"
+    return s, got
+
+
+def data(spec, name):
+    return np.asarray(spec.tensors[name].data, dtype=np.float64)
+
+
+# ------------------------------------------------------------------------------------------------ CacheWrite
+def check_written(spec):
+    _, got = run(spec)
+    for n, want in run_graph(spec).items():
+        np.testing.assert_array_equal(got[n], want, err_msg=n)      # rows are copied, or quantised by correctly rounded quotients
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("T,first,count", [(1, [0, 7, 8, 47], None), (1, [47, 48, -1, 3], None), (11, [0, 5, 36, 40], [11, 0, 11, 3]),
+                                           (29, [-4, 13, 2000000000, -2147483648], [29, 40, 7, 29])])
+def test_write(dtype, cache, T, first, count):
+    check_written(dg.write_graph(dtype, cache, T, first, count))
+
+
+@pytest.mark.parametrize("DK,DV,HK,S", [(16, 16, 1, 1), (48, 80, 3, 5), (256, 16, 2, 64), (128, 128, 5, 40), (80, 256, 1, 100)])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("f32", "f32")])
+def test_write_shapes(dtype, cache, DK, DV, HK, S):
+    check_written(dg.write_graph(dtype, cache, 2 * S + 3, [1, 0, S - 1], [2 * S + 3, 2 * S, 1], HK=HK, DK=DK, DV=DV, S=S, M=4))
+
+
+def test_write_leaves_out_pages_that_are_not_there():
+    table = np.array([[0, -1, 3, 99, 2, 1], [4, 5, 6, 7, -2147483648, 2147483647]])
+    check_written(dg.write_graph("bf16", "bf16", 40, [3, 1], table=table, P=8))
+    check_written(dg.write_graph("bf16", "i8", 40, [3, 1], table=table, P=8))
+
+
+@pytest.mark.parametrize("cache", ["f16", "i8"])
+def test_a_slot_written_twice_keeps_the_last(cache):
+    # two sequences on the same pages, one sequence with a page twice in its row, and one that meets neither
+    table = np.array([[0, 1, 2, 0, 1, 1], [2, 1, 0, 3, 3, 3], [4, 5, 6, 7, 8, 9]])
+    check_written(dg.write_graph("f16", cache, 44, [2, 0, 1], [44, 17, 30], table=table, P=10))
+    check_written(dg.write_graph("f16", cache, 1, [3, 19, 3], table=table, P=10))
+
+
+def test_rows_at_the_ends_of_the_range_of_a_step():
+    k = dg.normal(3, 1, (6, 1, 2, 32), "f32").astype(np.float32)
+    k[0] = 0.0
+    k[1, 0, 0, 3], k[1, 0, 1, 5] = np.inf, np.nan
+    k[2] *= np.float32(1e-37)
+    k[3] *= np.float32(3e37)
+    k[4, 0, 0] = np.float32(2.0 ** -120)
+    k[4, 0, 1] = np.float32(2.0 ** -119)
+    k[5, 0, 0, :] = np.arange(32) - 15.5           # values in the middle between two whole numbers of the step
+    k[5, 0, 0, 0] = 127.0
+    check_written(dg.write_graph("f32", "i8", 1, [0, 1, 2, 3, 4, 5], k=k, v=k))
+
+
+# ------------------------------------------------------------------------------------------------ CacheRead
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("L,held,HK,DK,DV,S", [(1, [0, 1, 5], 2, 32, 32, 8), (41, [41, 17, -3], 3, 48, 80, 5), (70, [100, 48, 9], 1, 256, 16, 16), (48, [8, 16, 2000000000], 4, 128, 128, 8)])
+def test_read(dtype, cache, L, held, HK, DK, DV, S):
+    spec = dg.read_graph(dtype, cache, held, L, HK=HK, DK=DK, DV=DV, S=S)
+    _, got = run(spec)
+    for n, want in run_graph(spec).items():
+        if cache != "i8":
+            np.testing.assert_array_equal(got[n], want, err_msg=n)
+        else:      # one product in 32 bits, one rounding to the result's type
+            assert np.all(np.abs(got[n] - want) <= np.abs(want) * (dg.HALF_STEP[dtype] + 2.0 ** -24 * 1.01)), n
+
+
+def test_read_of_pages_that_are_not_there():
+    table = np.array([[0, -1, 3, 99, 2, 1], [4, 5, 6, 7, -2147483648, 2147483647]])
+    spec = dg.read_graph("bf16", "bf16", [48, 48], 48, table=table)
+    _, got = run(spec)
+    for n, want in run_graph(spec).items():
+        np.testing.assert_array_equal(got[n], want)
+
+
+# ------------------------------------------------------------------------------------------------ CacheAttention
+def check_attention(spec, got=None):
+    """|o - o64| <= u |o64| + c sum_j p_j |v_j|: u is the rounding of the result; c what each probability may be off by,
+    relatively - its own rounding to the operand of the second product (16-bit pools; twice, for the sum's share), and the
+    error of its score, (channels + 8) roundings of 2^-24 of sum |q k|, the exponential's 2 and the sums' one per key."""
+    if got is None:
+        _, got = run(spec)
+    op = spec.ops[0]
+    want = run_graph(spec)["o"]
+    q, pools = data(spec, op.inputs[0]), [data(spec, n) for n in op.inputs[1:-2]]
+    size = dg.GraphBuilder("size", spec.dtype)
+    size.g.tensors, size.g.ops = dict(spec.tensors), [op]
+    magnitude = run_graph(size.g, feeds={op.inputs[2]: np.abs(pools[1])})["o"]
+    kmax = np.abs(pools[0] * (pools[2][..., None] if len(pools) == 4 else 1.0)).max()
+    score = np.abs(q).sum(-1).max() * kmax * abs(op.attrs.get("scale", 1.0 / np.sqrt(q.shape[-1])))
+    keys = spec.tensors[op.inputs[-2]].shape[1] * pools[0].shape[2]
+    p16 = 2 * dg.HALF_STEP[spec.dtype] if len(pools) == 2 and spec.dtype != "f32" else 0.0
+    c = p16 + 2.0 ** -24 * (2 * (q.shape[-1] + 8) * score + 16 + keys)
+    off = np.abs(got["o"] - want) - (dg.HALF_STEP[spec.dtype] * np.abs(want) * (1 + 2.0 ** -8) + c * magnitude)
+    assert np.all(off <= 0), f"{spec.name}: {off.max():.3e} over its bound"
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("HQ,HK,DK,DV,S,M,held", [
+    (4, 4, 64, 64, 16, 8, [1, 2, 31, 32, 33, 128, 0]),
+    (8, 2, 128, 128, 16, 40, [640, 129, 300]),
+    (7, 1, 48, 80, 5, 13, [65, 64, 1]),
+    (34, 2, 96, 16, 20, 7, [140, 77]),          # more than sixteen query heads a key head
+    (3, 3, 256, 256, 1, 150, [150, 5]),
+    (32, 2, 32, 112, 64, 3, [192, 100]),
+    (6, 6, 16, 32, 100, 2, [200, 101, 99]),
+])
+def test_attention(dtype, cache, HQ, HK, DK, DV, S, M, held):
+    check_attention(dg.attend_graph(dtype, cache, held, HQ, HK, DK, DV, S, M))
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "i8"), ("f32", "f32")])
+@pytest.mark.parametrize("window", [1, 5, 32, 33, 200, 100000])
+def test_attention_window(dtype, cache, window):
+    check_attention(dg.attend_graph(dtype, cache, [1, 40, 257, 512, 300], S=16, M=32, attrs={"window": window}))
+
+
+@pytest.mark.parametrize("scale", [0.5, -0.25, 0.0, 3.0])
+def test_attention_scale(scale):
+    check_attention(dg.attend_graph("f16", "f16", [100, 17], S=16, M=8, attrs={"scale": scale}))
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32"), ("f16", "i8")])
+def test_attention_split_over_long_sequences(dtype, cache):
+    # one sequence of thousands of keys among short and empty ones: split, joined, and splits that nothing is left for
+    check_attention(dg.attend_graph(dtype, cache, [5000, 3, 0, 1300], HQ=4, HK=1, DK=64, DV=64, S=16, M=313))
+
+
+def test_attention_over_capacity_and_below_zero():
+    check_attention(dg.attend_graph("bf16", "bf16", [2147483647, -5, -2147483648, 129], S=16, M=8))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "i8"])
+@pytest.mark.parametrize("S", [16, 5])
+def test_attention_sees_only_pages_that_are_there(cache, S):
+    table, P = dg.pages_of(5, 3, 12)
+    table[0, 3], table[0, 5], table[1, :], table[2, 11] = -1, P, -7, 2147483647
+    spec = dg.attend_graph("bf16", cache, [12 * S, 12 * S, 12 * S], S=S, M=12, table=table, P=P)
+    _, got = run(spec)
+    assert np.all(got["o"][1] == 0.0)
+    check_attention(spec, got)
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "i8")])
+def test_what_masked_slots_hold_does_not_matter(dtype, cache):
+    """Slots behind a sequence's keys, slots before its window and pages that no table names hold infinities and NaN."""
+    held, S, M = [37, 100, 1, 0], 16, 8
+    spec = dg.attend_graph(dtype, cache, held, S=S, M=M, attrs={"window": 50})
+    want = run(spec)[1]["o"]
+    table = spec.tensors["table"].data
+    seen = np.zeros(spec.tensors["k_pool"].shape[0] * S, dtype=bool).reshape(-1, S)
+    for b, n in enumerate(held):
+        for p in range(max(0, n - 50), n):
+            seen[table[b, p // S], p % S] = True
+    names = ["k_scale", "v_scale"] if cache == "i8" else ["k_pool", "v_pool"]
+    for i, n in enumerate(names):
+        t = spec.tensors[n]
+        t.data = np.array(t.data)
+        bad = np.where(np.arange(t.data.size).reshape(t.data.shape) % 3 == 0, np.nan, np.inf if i else -np.inf)
+        m = seen[:, None, :] if cache == "i8" else seen[:, None, :, None]
+        t.data = np.where(m, t.data, bad)
+    np.testing.assert_array_equal(run(spec)[1]["o"], want)
+
+
+def test_scores_far_apart():
+    # a later key far above all earlier ones (the reference moves), probabilities that vanish, and scores of tens of thousands
+    for std in (10.0, 300.0):
+        spec = dg.attend_graph("f32", "f32", [400, 33], HQ=2, HK=1, DK=64, DV=32, S=16, M=25, q_std=std)
+        check_attention(spec)
+
+
+def test_a_pool_beyond_32_bits():
+    """Rows whose element offsets pass 2^31 and 2^32, through all three operators (as torch tensors: 8 GiB a pool)."""
+    import torch
+
+    from paper_2108_13342_amd import api
+
+    HK, S, D = 4, 64, 128
+    P = (1 << 32) // (HK * S * D) + 40
+    dev = torch.device("cuda:0")
+    k, v = (torch.zeros((P, HK, S, D), dtype=torch.float16, device=dev) for _ in range(2))
+    table = torch.tensor([[P - 1, 7, P - 2, P // 2 + 3]], dtype=torch.int32, device=dev)
+    T = 4 * S - 5
+    gen = torch.Generator(device=dev).manual_seed(3)
+    fresh = [torch.randn((1, T, HK, D), generator=gen, device=dev).half() for _ in range(2)]
+    q = torch.randn((1, HK, D), generator=gen, device=dev).half()
+    first, held = torch.zeros(1, dtype=torch.int32, device=dev), torch.full((1,), T, dtype=torch.int32, device=dev)
+    out = [torch.empty((1, T, HK, D), dtype=torch.float16, device=dev) for _ in range(2)] + [torch.empty((1, HK, D), dtype=torch.float16, device=dev)]
+    g = api.Graph()
+    tin = [k, v, *fresh, table, first, held, q]
+    ids = [g.add_tensor(f"i{n}", {torch.float16: "f16", torch.int32: "i32"}[t.dtype], t.shape, "input") for n, t in enumerate(tin)]
+    outs = [g.add_tensor(f"o{n}", "f16", t.shape, "output") for n, t in enumerate([k, v] + out)]
+    g.add_op("CacheWrite", ids[:6], outs[:2])
+    g.add_op("CacheRead", outs[:2] + [ids[4], ids[6]], outs[2:4], {"length": T})
+    g.add_op("CacheAttention", [ids[7]] + outs[:2] + [ids[4], ids[6]], outs[4:5])
+    g.finalize()
+    stream = torch.cuda.current_stream().cuda_stream
+    plan = api.Plan(g, [], stream=stream)
+    ws = torch.empty(max(plan.workspace_bytes(), 256), dtype=torch.uint8, device=dev)
+    plan.prepare(ws.data_ptr(), stream)
+    plan.run([t.data_ptr() for t in tin], [t.data_ptr() for t in [k, v] + out], ws.data_ptr(), stream)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], fresh[0]) and torch.equal(out[1], fresh[1])
+    s = (fresh[0][0].double() * q.double()).sum(-1) / D ** 0.5
+    want = (torch.softmax(s, 0)[..., None] * fresh[1][0].double()).sum(0)
+    assert (out[2][0].double() - want).abs().max() <= 4e-3      # |v| <= 5: two roundings of 2^-11 of the probabilities, sums and result below that
+
+
+# ------------------------------------------------------------------------------------------------ MatMulInt4
+def check_int4(spec, **kw):
+    """|y - y64| <= u |y64| + 2^-24 (K + 16) sum_k |x_k| 62 s: u the rounding of the result (and, where every operator is a kernel of
+    its own, that of the product), and fp32 sums over K of terms up to |x| (16 + 15 and, for the zero point, 16 + 15) s."""
+    _, got = run(spec, **kw)
+    env = run_graph(spec, keep="all")
+    x, s = data(spec, "x"), data(spec, "s")
+    K = x.shape[-1]
+    terms = np.abs(x) @ np.repeat(s, spec.ops[0].attrs["group_size"], axis=1)[:, :K].T
+    for n, y in got.items():
+        rounded = np.abs(env[n]) + (np.abs(env[spec.ops[0].outputs[0]]) if kw.get("fusion") == 0 and len(spec.ops) > 1 else 0.0)
+        off = np.abs(y - env[n]) - (dg.HALF_STEP[spec.dtype] * rounded * (1 + 2.0 ** -7) + 2.0 ** -24 * (K + 16) * 62 * terms)
+        assert np.all(off <= 0), f"{n}: {off.max():.3e} over its bound"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K,N,G,zeros", [(1, 1, 1, 32, False), (1, 31, 5, 32, True), (1, 128, 16, 128, False), (1, 129, 33, 64, True), (1, 768, 2304, 64, False),
+                                           (3, 96, 40, 96, True), (16, 256, 64, 256, True), (17, 200, 100, 32, False), (33, 321, 47, 96, True),
+                                           (64, 1024, 130, 128, True), (65, 130, 70, 64, True), (150, 64, 1100, 32, False), (2, 4000, 24, 4096, True),
+                                           (5, 2049, 9000, 128, True)])
+def test_int4(dtype, M, K, N, G, zeros):
+    check_int4(dg.int4_graph(dtype, (M,), K, N, G, zeros))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lead", [(1, 1), (2, 3), (2, 2, 5)])
+def test_int4_with_what_follows_it(dtype, lead):
+    check_int4(dg.int4_graph(dtype, lead, 160, 72, 32, True, bias=True))
+    check_int4(dg.int4_graph(dtype, lead, 160, 72, 32, True, bias=True), fusion=0)
+
+
+def test_every_code_and_zero_point():
+    """Each of the 16 codes against each of the 16 zero points, exactly: x of ones and twos, a scale of one half."""
+    for dtype in ("f32", "f16", "bf16"):
+        spec = dg.int4_graph(dtype, (2,), 32, 256, 32, True)
+        n = np.arange(256)
+        spec.tensors["w"].data = np.repeat(((n % 16) * 17)[:, None], 16, axis=1)
+        spec.tensors["z"].data = (n // 16)[:, None]
+        spec.tensors["s"].data = np.full((256, 1), 0.5)
+        spec.tensors["x"].data = np.stack([np.eye(32)[3], 2 * np.eye(32)[30]])
+        want = np.stack([(n % 16 - n // 16) * 0.5, (n % 16 - n // 16) * 1.0])
+        _, got = run(spec)
+        np.testing.assert_array_equal(next(iter(got.values())), want)
+
+
+def test_int4_large_and_tiny_activations():
+    spec = dg.int4_graph("f32", (2,), 96, 50, 32)
+    for scale in (1e-30, 1e30):
+        spec.tensors["x"].data = dg.normal(4, 1, (2, 96), "f32") * np.float32(scale)
+        check_int4(spec)
+
+
+# ------------------------------------------------------------------------------------------------ together
+def rounded_graph(spec):
+    """The oracle with every operator's result rounded to its storage type."""
+    from oracle.interp import eval_op
+    from workloads import rng
+
+    env = {t.name: np.asarray(t.data).astype(np.int64 if t.dtype[0] in "iu" else np.float64) for t in spec.tensors.values() if t.data is not None}
+    for op in spec.ops:
+        res = eval_op(op.kind, [env[i] for i in op.inputs], op.attrs)
+        for n, v in zip(op.outputs, res if isinstance(res, (list, tuple)) else [res]):
+            d = spec.tensors[n].dtype
+            env[n] = rng.round_to(np.asarray(v, dtype=np.float64), d).astype(np.float64) if d in dg.HALF_STEP else np.asarray(v, dtype=np.float64)
+    return env
+
+
+@pytest.mark.parametrize("cache", ["bf16", "i8"])
+@pytest.mark.parametrize("fusion", [0, 1])
+def test_decode_step_of_a_stack(cache, fusion):
+    """One step of a two-layer decoder stack against the oracle.  The storage roundings of the operators' results alone (the oracle
+    with them, against the oracle) move the logits by 1.9e-2 of their size and the new rows by up to 6e-3; the executor rounds at the
+    same places, or at fewer, other values than these: twice that distance.  A row of 8 bits moves by whole steps."""
+    from parity import rel_err
+    from workloads import configs
+
+    spec = configs.gpt2_decode_step(**configs.SMALL_EXTRA["gpt2_decode_step"], cache=cache)
+    want, near = run_graph(spec), rounded_graph(spec)
+    _, got = run(spec, fusion=fusion)
+    for n, w in want.items():
+        if cache == "i8" and n.endswith(("k_new", "v_new")):
+            scale = n.replace("_new", "_scale_new")
+            x, y, z = (e[n] * e[scale][..., None] for e in (got, want, near))
+            assert np.all(np.abs(x - y) <= 2 * np.abs(z - y).max() + want[scale][..., None]), n
+        else:
+            assert rel_err(got[n], w) <= 2 * rel_err(near[n], w), n
+
+
+@pytest.mark.parametrize("cache", ["f16", "i8"])
+def test_tokens_generated_one_by_one(cache):
+    """A cache filled token by token gives what one filled at once gives, bit for bit, and each step attends over what is there."""
+    import torch
+
+    from paper_2108_13342_amd import api
+
+    T, HK, HQ, D, S, M, B = 37, 2, 4, 64, 8, 5, 2
+    whole = dg.write_graph("f16", cache, T, [0, 0], HK=HK, DK=D, DV=D, S=S, M=M)
+    _, once = run(whole)
+    k, v = (np.asarray(whole.tensors[n].data) for n in "kv")
+
+    # one graph for a step: write the token, attend over all up to it
+    spec = dg.write_graph("f16", cache, 1, [0, 0], HK=HK, DK=D, DV=D, S=S, M=M, k=k[:, :1], v=v[:, :1])
+    b = dg.GraphBuilder("step", "f16")
+    b.g = spec
+    q = b.input("q", (B, HQ, D), dg.normal(9, 1, (B, HQ, D), "f16"))
+    kept = list(spec.ops[0].outputs)
+    held = b.input("held", (B,), np.array([1, 1]), dtype="i32")
+    b.g.ops.append(dg.OpSpec("CacheAttention", [q] + kept + ["table", held], [b._add("o", "f16", (B, HQ, D), "output")]))
+    s = api.Session(spec, guard_bytes=256)
+    at = {t.name: s.inputs[0][i] for i, t in enumerate(t for t in spec.tensors.values() if t.kind == "input")}
+    for t in range(T):
+        at["k"].copy_(torch.from_numpy(k[:, t:t + 1]))
+        at["v"].copy_(torch.from_numpy(v[:, t:t + 1]))
+        at["first"].fill_(t)
+        at["held"].fill_(t + 1)
+        s.run()
+        if t in (0, 7, 8, T - 1):
+            got = s.result()
+            now = dg.attend_graph("f16", cache, [t + 1] * B, HQ, HK, D, D, S, M, attrs={}, P=spec.tensors["k_pool"].shape[0])
+            for n in kept:
+                now.tensors[n.replace("_new", "")].data = got[n]
+            now.tensors["q"].data, now.tensors["table"].data = spec.tensors["q"].data, spec.tensors["table"].data
+            check_attention(now, {"o": got["o"]})
+    got = s.result()
+    assert s.guards_intact()
+    for n, w in once.items():
+        np.testing.assert_array_equal(got[n], w, err_msg=n)
+
+
+def test_on_another_stream_and_replayed():
+    """A step recorded into a graph and replayed, with eager work between the replays, gives the eager results every time; the
+    buffers' new contents count."""
+    import torch
+
+    from paper_2108_13342_amd import api
+
+    spec = dg.attend_graph("bf16", "bf16", [3000, 40], HQ=4, HK=1, S=16, M=190)
+    s = api.Session(spec)
+    bound = s.plan.bind(s.in_ptrs(), s.out_ptrs(), s.workspace.data_ptr())
+    at = {t.name: s.inputs[0][i] for i, t in enumerate(t for t in spec.tensors.values() if t.kind == "input")}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        bound.run(side.cuda_stream)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            bound.run(torch.cuda.current_stream().cuda_stream)
+    for i, held in enumerate(([3000, 40], [1, 3040], [0, 2999], [777, 778])):
+        at["held"].copy_(torch.tensor(held, dtype=torch.int32))
+        at["q"].mul_(1.25)
+        s.outputs[0][0].fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = s.outputs[0][0].clone()
+        s.outputs[0][0].fill_(float("nan"))
+        bound.run(torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, s.outputs[0][0]), f"replay {i}"
+        assert torch.isfinite(replayed.float()).all()
+
+
+def test_two_runs_are_alike_bit_for_bit():
+    for spec in (dg.attend_graph("bf16", "i8", [2500, 900], HQ=8, HK=1, S=16, M=160), dg.int4_graph("f16", (3,), 1500, 200, 64, True)):
+        s, got = run(spec)
+        for _ in range(3):
+            s.run()
+            again = s.result()
+            for n in got:
+                np.testing.assert_array_equal(got[n], again[n])
+
+
+def test_in_place_results_take_their_operand_s_buffer():
+    from paper_2108_13342_amd import api
+
+    s = api.Session(dg.write_graph("bf16", "bf16", 1, [0, 3]))
+    ins, outs = s.in_ptrs(), s.out_ptrs()
+    with pytest.raises(api.DnnfError, match="in place"):
+        s.plan.run(ins, [outs[0], ins[2]], s.workspace.data_ptr(), s.stream)
+    with pytest.raises(api.DnnfError, match="share one buffer"):
+        s.plan.run([ins[0], ins[0]] + ins[2:], [ins[0], ins[0]], s.workspace.data_ptr(), s.stream)
+    s.plan.run(ins, outs, s.workspace.data_ptr(), s.stream)
+    s.result()
+
+
+def test_static_workspace():
+    from paper_2108_13342_amd import api
+
+    spec = dg.attend_graph("bf16", "bf16", [1500, 700], HQ=4, HK=1, S=16, M=100)
+    s, got = run(spec)
+    s.outputs[0][0].zero_()
+    s.plan.run_static(s.in_ptrs(), s.out_ptrs(), s.stream)
+    np.testing.assert_array_equal(s.result()["o"], got["o"])

@@ -1,0 +1,231 @@
+"""Operators of single-token inference, without a GPU: shapes, refusals, how their blocks are planned, and the oracle's definitions
+against plain loops."""
+import numpy as np
+import pytest
+
+import decode_graphs as dg
+from oracle.interp import run_graph
+from paper_2108_13342_amd import api
+
+
+def plan(spec, **kw):
+    g, _ = api.graph_from_spec(spec)
+    g.rewrite()
+    return api.Plan(g, [1] * len(spec.weights()), **kw)
+
+
+def kernels(p):
+    return [d["kernel_name"].split(":")[-1] for d in p.describe()]
+
+
+# ------------------------------------------------------------------------------------------------ the oracle
+def test_oracle_attention_against_loops():
+    spec = dg.attend_graph("f32", "i8", [9, 0, 21], HQ=6, HK=2, DK=16, DV=32, S=4, M=6, attrs={"window": 7})
+    t = {n: np.asarray(x.data, dtype=np.float64) for n, x in spec.tensors.items() if x.data is not None}
+    got = run_graph(spec)["o"]
+    for b, held in enumerate([9, 0, 21]):
+        for h in range(6):
+            num, den = np.zeros(32), 0.0
+            for p in range(max(0, held - 7), held):
+                at = (int(t["table"][b, p // 4]), h // 3, p % 4)
+                e = np.exp(np.dot(t["q"][b, h], t["k_pool"][at] * t["k_scale"][at]) / 4.0)
+                num, den = num + e * t["v_pool"][at] * t["v_scale"][at], den + e
+            np.testing.assert_allclose(got[b, h], num / den if held else 0.0, rtol=1e-12, atol=1e-15)
+
+
+def test_oracle_quantises_to_half_a_step():
+    spec = dg.write_graph("f32", "i8", 5, [2, 7])
+    out = run_graph(spec)
+    for b, first in enumerate((2, 7)):
+        for t in range(5):
+            page, slot = spec.tensors["table"].data[b, (first + t) // 8], (first + t) % 8
+            for n in "kv":
+                n8, step, x = out[f"{n}_pool_new"][page, :, slot], out[f"{n}_scale_new"][page, :, slot, None], np.asarray(spec.tensors[n].data)[b, t]
+                assert np.all(np.abs(n8) <= 127) and np.all(n8 == np.rint(n8)) and np.all(np.abs(n8).max(-1) == 127)
+                assert np.all(np.abs(n8 * step - x) <= step * (0.5 + 127 * 2.0 ** -23))
+
+
+def test_oracle_read_returns_what_was_written():
+    w = dg.write_graph("f32", "f32", 13, [0, 0], [13, 4], DK=16, DV=48)
+    pools = run_graph(w)
+    r = dg.read_graph("f32", "f32", [13, 4], 15, DK=16, DV=48)
+    out = run_graph(r, feeds={"k_pool": pools["k_pool_new"], "v_pool": pools["v_pool_new"]})
+    for n in "kv":
+        want = np.zeros((2, 15) + w.tensors[n].shape[2:])
+        want[0, :13], want[1, :4] = w.tensors[n].data[0], w.tensors[n].data[1, :4]
+        np.testing.assert_array_equal(out[n + "_out"], want)
+
+
+def test_oracle_int4_against_loops():
+    spec = dg.int4_graph("f32", (2,), 71, 3, 32, True)
+    t = {n: np.asarray(x.data, dtype=np.float64) for n, x in spec.tensors.items() if x.data is not None}
+    y = next(iter(run_graph(spec).values()))
+    for m in range(2):
+        for n in range(3):
+            s = 0.0
+            for k in range(71):
+                byte = int(t["w"][n, k // 2])
+                s += t["x"][m, k] * ((byte >> 4 if k % 2 else byte & 15) - t["z"][n, k // 32]) * t["s"][n, k // 32]
+            assert abs(y[m, n] - s) <= 1e-12 * 71
+
+
+# ------------------------------------------------------------------------------------------------ plans
+def test_blocks_of_a_decode_step():
+    from workloads import configs
+
+    p = plan(configs.gpt2_decode_step(**configs.SMALL_EXTRA["gpt2_decode_step"]))
+    ops = [d["ops"] for d in p.describe()]
+    # what follows a product runs in its kernel: bias, heads, residual sums, the activation
+    assert ["MatMulInt4", "Add", "Split", "Reshape", "Reshape", "Reshape"] in ops and ["MatMulInt4", "Add", "Add"] in ops
+    assert any(o[0] == "MatMulInt4" and "Tanh" in o for o in ops)
+    assert ops.count(["CacheWrite"]) == 2 and ops.count(["CacheAttention"]) == 2
+    # every attention stands behind the write that fills its pools
+    flat = [o[0] for o in ops]
+    assert [o for o in flat if o.startswith("Cache")] == ["CacheWrite", "CacheAttention"] * 2
+
+
+def test_short_capacity_takes_one_kernel_and_long_capacity_is_split():
+    assert kernels(plan(dg.attend_graph("bf16", "bf16", [9], M=8))) == ["cache_attend_split1_16"]
+    info = plan(dg.attend_graph("bf16", "bf16", [9], M=80)).describe()[0]
+    assert info["n_kernel_launches"] == 2 and "split10_" in info["kernel_name"]
+    # a window bounds what there is to split
+    assert kernels(plan(dg.attend_graph("bf16", "bf16", [9], M=80, attrs={"window": 90}))) == ["cache_attend_split1_16"]
+
+
+def test_mapping_types_and_families():
+    assert api.op_kind_mapping_type("CacheRead") == api.MAPPING_NAMES.index("One-to-Many")
+    for k in ("CacheWrite", "CacheAttention", "MatMulInt4"):
+        assert api.op_kind_mapping_type(k) == api.MAPPING_NAMES.index("Many-to-Many")
+    assert api.FAMILY_NAMES[plan(dg.attend_graph("bf16", "bf16", [9])).describe()[0]["family"]] == "cache"
+    assert api.FAMILY_NAMES[plan(dg.int4_graph("f16", (1,), 64, 64, 32)).describe()[0]["family"]] == "int4-gemm"
+
+
+def test_casts_next_to_typed_operands_stay():
+    """A cast in front of or behind these operators is part of their types and is not merged away by the rewriting."""
+    b = dg.GraphBuilder("cast", "f32")
+    spec = dg.int4_graph("f32", (2,), 64, 48, 32)
+    b.g = spec
+    x16 = b.input("x16", (2, 64), dg.normal(1, 1, (2, 64), "f16"), dtype="f16")
+    spec.ops[0].inputs[0] = b.op("Cast", [x16], (2, 64), {"to": 1})
+    y = spec.ops[0].outputs[0]
+    spec.tensors[y].kind = "intermediate"
+    b.g.ops = [spec.ops[1], spec.ops[0]]
+    y16 = b.op("Cast", [y], (2, 48), {"to": 10}, out_dtype="f16")
+    b.mark_output(y16)
+    del spec.tensors["x"]
+    g, _ = api.graph_from_spec(spec)
+    g.rewrite()
+    assert [k for _, k, _ in g.live_ops()].count("Cast") == 2
+    api.Plan(g, [1] * 2)
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+def refused(spec, match, code=None):
+    with pytest.raises(api.DnnfError, match=match) as e:
+        api.graph_from_spec(spec)
+    assert code is None or e.value.code == code
+
+
+def retyped(spec, name, dtype):
+    spec.tensors[name].dtype = dtype
+    return spec
+
+
+def reshaped(spec, name, shape):
+    spec.tensors[name].shape, spec.tensors[name].data = shape, None
+    return spec
+
+
+def with_attrs(spec, **kw):
+    spec.ops[0].attrs.update(kw)
+    return spec
+
+
+INVALID, MISMATCH, UNSUPPORTED = -1, -2, -3
+
+
+@pytest.mark.parametrize("spec,match,code", [
+    (lambda: reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "q", (2, 3, 64)), "no multiple of the key heads", MISMATCH),
+    (lambda: reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "q", (2, 4, 32)), "channels of a key", MISMATCH),
+    (lambda: reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "held", (3,)), "one number per sequence", MISMATCH),
+    (lambda: reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "table", (16,)), "table", MISMATCH),
+    (lambda: reshaped(dg.attend_graph("bf16", "i8", [1, 1]), "v_scale", (5, 2, 16)), "scale tensor", MISMATCH),
+    (lambda: reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "v_pool", (19, 2, 8, 64)), "pools differ", MISMATCH),
+    (lambda: dg.attend_graph("bf16", "bf16", [1, 1], DK=40), "multiple of 16", UNSUPPORTED),
+    (lambda: dg.attend_graph("bf16", "bf16", [1, 1], DV=272), "at most 256", UNSUPPORTED),
+    (lambda: retyped(dg.attend_graph("bf16", "bf16", [1, 1]), "q", "f16"), "share one type", INVALID),
+    (lambda: retyped(dg.attend_graph("bf16", "bf16", [1, 1]), "held", "i64"), "I32", INVALID),
+    (lambda: retyped(dg.attend_graph("bf16", "bf16", [1, 1]), "v_pool", "f16"), "share one type", INVALID),
+    (lambda: retyped(dg.attend_graph("bf16", "i8", [1, 1]), "k_scale", "bf16"), "F32", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": -1}), "window", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": 2.5}), "window", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"scale": float("nan")}), "scale", INVALID),
+    (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=0), "length", INVALID),
+    (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=5), "declared", MISMATCH),
+    (lambda: retyped(dg.read_graph("f16", "f16", [1], 4), "k_out", "f32"), "share one type", INVALID),
+    (lambda: retyped(dg.write_graph("f16", "f16", 1, [1]), "k", "f32"), "share one type", INVALID),
+    (lambda: retyped(dg.write_graph("f16", "f16", 1, [1]), "k_pool_new", "bf16"), "differs in type", INVALID),
+    (lambda: dg.int4_graph("f16", (1,), 64, 8, 16), "group_size", INVALID),
+    (lambda: dg.int4_graph("f16", (1,), 64, 8, 48), "group_size", INVALID),
+    (lambda: reshaped(dg.int4_graph("f16", (1,), 64, 8, 32), "w", (8, 31)), "bytes", MISMATCH),
+    (lambda: reshaped(dg.int4_graph("f16", (1,), 64, 8, 32), "s", (8, 3)), "groups of K", MISMATCH),
+    (lambda: retyped(dg.int4_graph("f16", (1,), 64, 8, 32), "s", "f32"), "share a float type", INVALID),
+    (lambda: retyped(dg.int4_graph("f16", (1,), 64, 8, 32), "w", "i8"), "U8", INVALID),
+    (lambda: retyped(dg.int4_graph("f16", (1,), 64, 8, 32, True), "z", "i8"), "U8", INVALID),
+])
+def test_refusals(spec, match, code):
+    refused(spec(), match, code)
+
+
+def test_operand_counts():
+    spec = dg.attend_graph("bf16", "bf16", [1])
+    spec.ops[0].inputs.append("held")
+    refused(spec, "too many operands", INVALID)
+    spec = dg.attend_graph("bf16", "bf16", [1])
+    spec.ops[0].inputs.pop()
+    refused(spec, "no operand for held", INVALID)
+    spec = dg.write_graph("bf16", "i8", 1, [1])
+    spec.ops[0].outputs.pop()
+    refused(spec, "has 4 results", INVALID)
+
+
+def test_pools_are_inputs_updated_in_place():
+    spec = dg.write_graph("bf16", "bf16", 1, [1])
+    spec.tensors["k_pool"].kind = "weight"
+    refused(spec, "must be an INPUT", INVALID)
+    spec = dg.write_graph("bf16", "bf16", 1, [1])
+    spec.tensors["v_pool_new"].kind = "intermediate"
+    refused(spec, "must be an INPUT", INVALID)
+    # nobody else reads the pool under the name it had before
+    spec = dg.write_graph("bf16", "bf16", 1, [1])
+    b = dg.GraphBuilder("reader", "bf16")
+    b.g = spec
+    held = b.input("held", (1,), np.array([1]), dtype="i32")
+    b.g.ops.append(dg.OpSpec("CacheRead", ["k_pool", "v_pool_new", "table", held], [b._add(n, "bf16", (1, 4, 2, 32), "output") for n in ("ko", "vo")], {"length": 4}))
+    refused(spec, "other operators read its result", INVALID)
+    # one pool as keys and values at once
+    spec = dg.write_graph("bf16", "bf16", 1, [1])
+    spec.ops[0].inputs[1] = "k_pool"
+    refused(spec, "other operators read its result", INVALID)
+
+
+def test_other_operators_refuse_tensors_of_8_bits():
+    b = dg.GraphBuilder("other", "f32")
+    x = b.input("x", (4, 4), np.zeros((4, 4)), dtype="i8")
+    b.mark_output(b.op("Relu", [x], (4, 4), out_dtype="i8"))
+    refused(b.finish(), "8 bits", UNSUPPORTED)
+
+
+def test_sizes_beyond_the_index_ranges():
+    def declared(P, S, M, T=1):
+        g = api.Graph()
+        pools = [g.add_tensor(n, "bf16", (P, 8, S, 128), "input") for n in "kv"]
+        rest = [g.add_tensor("q", "bf16", (1, 8, 128), "input"), g.add_tensor("t", "i32", (1, M), "input"), g.add_tensor("h", "i32", (1,), "input")]
+        g.add_op("CacheAttention", [rest[0]] + pools + rest[1:], [g.add_tensor("o", "bf16", (1, 8, 128), "output")])
+        g.finalize()
+
+    declared(1 << 20, 128, 1 << 16)
+    with pytest.raises(api.DnnfError, match="2\\^31 rows"):
+        declared(1 << 24, 16, 4)
+    with pytest.raises(api.DnnfError, match="2\\^30 positions"):
+        declared(16, 1024, 1 << 20)

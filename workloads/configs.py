@@ -17,7 +17,7 @@ import math
 import numpy as np
 
 from . import rng
-from .graph import GraphBuilder, bcast_shape
+from .graph import GraphBuilder, OpSpec, bcast_shape
 
 BASE_SEED = 210813342
 
@@ -395,6 +395,52 @@ def gpt2_decoder(B=4, S=1024, D=768, NH=12, F=3072, L=12, V=50257, P=1024, dtype
     return b.finish()
 
 
+def gpt2_decode_step(B=8, D=768, NH=12, L=12, V=50257, held=1000, P=1024, page=16, G=64, dtype="bf16", cache="i8", seed=BASE_SEED + 7):
+    """One new token for each of B sequences through a decoder stack of gpt2_decoder's shape: the step that follows a prompt.
+    Every layer's keys and values are kept in pages of `page` slots (in `cache`, the storage type of the pools), P positions a
+    sequence; weights of the linear layers are 4-bit codes with a scale per G.  `held` keys are in the cache beforehand (fewer
+    for the later sequences)."""
+    st = _Streams(seed)
+    b = GraphBuilder("gpt2_decode_step", dtype)
+    hd, per = D // NH, (P + page - 1) // page
+    pages = B * per
+    before = np.maximum(0, held - (np.arange(B) * held) // (2 * B)).astype(np.int64)
+    ids = b.input("input_ids", (B,), st.integers((B,), 0, V), dtype="i64")
+    first = b.input("position", (B,), before, dtype="i32")
+    n_held = b.input("held", (B,), before + 1, dtype="i32")
+    order = np.argsort(rng.uniform(seed, 9999, (pages,)), kind="stable").astype(np.int64)
+    table = b.input("table", (B, per), order.reshape(B, per), dtype="i32")
+    wte = b.weight("wte", (V, D), st.normal((V, D), 0.0, 0.02, dtype))
+    wpe = b.weight("wpe", (P, D), st.normal((P, D), 0.0, 0.02, dtype))
+
+    def lin4(name, inp, k, n, bias=True):
+        w = b.weight(f"{name}_w", (n, (k + 1) // 2), st.integers((n, (k + 1) // 2), 0, 256), dtype="u8")
+        s = b.weight(f"{name}_s", (n, -(-k // G)), st.uniform((n, -(-k // G)), 0.002, 0.006, dtype))
+        y = b.op("MatMulInt4", [inp, w, s], b.shape(inp)[:-1] + (n,), {"group_size": G})
+        return _bin(b, "Add", y, b.weight(f"{name}_b", (n,), st.normal((n,), 0.0, 0.02, dtype))) if bias else y
+
+    h = _bin(b, "Add", b.op("Gather", [wte, ids], (B, D), {"axis": 0}), b.op("Gather", [wpe, first], (B, D), {"axis": 0}))
+    for l in range(L):
+        qkv = lin4(f"l{l}_attn", _layernorm_fp32(b, st, h, D, dtype, f"l{l}_ln1"), D, 3 * D)
+        q, k, v = b.op("Split", [qkv], [(B, D)] * 3, {"axis": 1, "split": [D, D, D]})
+        k, v = _reshape(b, k, (B, 1, NH, hd)), _reshape(b, v, (B, 1, NH, hd))
+        pools = []
+        for n in ("k", "v"):
+            data = st.integers((pages, NH, page, hd), -127, 128) if cache == "i8" else st.normal((pages, NH, page, hd), 0.0, 0.6, dtype)
+            pools.append(b.input(f"l{l}_{n}", (pages, NH, page, hd), data, dtype=cache))
+        if cache == "i8":
+            pools += [b.input(f"l{l}_{n}_scale", (pages, NH, page), st.uniform((pages, NH, page), 0.005, 0.015, "f32"), dtype="f32") for n in ("k", "v")]
+        kept = [b._add(f"{p}_new", b.g.tensors[p].dtype, b.shape(p), "output") for p in pools]
+        b.g.ops.append(OpSpec("CacheWrite", pools + [k, v, table, first], kept))
+        o = b.op("CacheAttention", [_reshape(b, q, (B, NH, hd))] + kept + [table, n_held], (B, NH, hd))
+        h = _bin(b, "Add", h, lin4(f"l{l}_proj", _reshape(b, o, (B, D)), D, D))
+        f = lin4(f"l{l}_fc", _layernorm_fp32(b, st, h, D, dtype, f"l{l}_ln2"), D, 4 * D)
+        f = _gelu_tanh(b, f, f"l{l}_gelu", pow_in_fp32=dtype != "f32")
+        h = _bin(b, "Add", h, lin4(f"l{l}_fcproj", f, 4 * D, D))
+    b.mark_output(lin4("head", _layernorm_fp32(b, st, h, D, dtype, "lnf"), D, V, bias=False))
+    return b.finish()
+
+
 def copy_calibration(N=16, C=256, H=64, W=64, seed=BASE_SEED + 9):
     """One elementwise operator over a tensor of the chain config's size: a plain streaming kernel of
     known traffic (64 MiB read, 64 MiB written) used to calibrate HBM byte counters."""
@@ -461,8 +507,9 @@ SMALL_HEAD32 = {
 }
 
 # workloads beyond the five benchmark configurations (bench.py --workload NAME)
-EXTRA = {"unet_decoder": unet_decoder}
-SMALL_EXTRA = {"unet_decoder": dict(N=2, C=32, R=6, steps=2)}
+EXTRA = {"unet_decoder": unet_decoder, "gpt2_decode_step": gpt2_decode_step}
+SMALL_EXTRA = {"unet_decoder": dict(N=2, C=32, R=6, steps=2),
+               "gpt2_decode_step": dict(B=3, D=96, NH=2, L=2, V=211, held=50, P=72, page=8, G=32)}
 
 CONFIGS = {
     "residual_block": residual_block,

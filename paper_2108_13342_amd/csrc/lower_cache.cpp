@@ -189,7 +189,8 @@ const char* kAttendBody = R"KRN(
 #define KV (DK % 64 == 0 ? 16 : 8)
 #endif
 #define NC ((DK + 4 * KV - 1) / (4 * KV))          // steps along a key's channels: four quarters of KV each
-typedef pool_t kvec_t __attribute__((ext_vector_type(KV)));
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+typedef pool_t krow_t __attribute__((ext_vector_type(KV)));
 
 // ---- operands of the two products
 #if POOL == 0
@@ -212,38 +213,80 @@ DEV void span_of(const int b, const int split, const int* __restrict__ held, int
   s1 = min(s0 + per, steps);
 }
 
-template <int VW> struct vvec { typedef pool_t t __attribute__((ext_vector_type(VW))); };
-template <> struct vvec<1> { typedef pool_t t; };
-template <int VW> DEV pool_t pick(const typename vvec<VW>::t& v, int e) { if constexpr (VW == 1) return v; else return v[e]; }
+// Rows that wait for their turn are held as 32-bit words (as vectors of small elements the compiler would give each element of
+// a loop-carried value a register of its own).
+template <int BYTES> struct words { typedef u32 t __attribute__((ext_vector_type(BYTES / 4))); };
+template <> struct words<4> { typedef u32 t; };
+template <> struct words<2> { typedef u16 t; };
+template <> struct words<1> { typedef unsigned char t; };
+template <int VW> struct vvec { typedef typename words<VW * (int)sizeof(pool_t)>::t t; typedef pool_t e __attribute__((ext_vector_type(VW))); };
+template <> struct vvec<1> { typedef typename words<(int)sizeof(pool_t)>::t t; typedef pool_t e __attribute__((ext_vector_type(1))); };
 
-// O^T += V^T . P^T for the channels BASE + 16 VW of a lane's eight keys
-template <int BASE, int VW, int T0> DEV void values(f32x4* o, const pool_t* __restrict__ vp, const long long (&vrow)[8], const u32 seen, const pfrag_t (&p)[PN], const int n, const int h) {
-  typedef typename vvec<VW>::t vec_t;
-  vec_t x[8];
+// the channels BASE + VW n .. of a lane's eight keys
+template <int BASE, int VW> DEV void load_values(typename vvec<VW>::t (&x)[8], const pool_t* __restrict__ vp, const long long (&vrow)[8], const int n) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = *(const vec_t*)(vp + vrow[j] * DV + BASE + n * VW);
+  for (int j = 0; j < 8; ++j) x[j] = *(const typename vvec<VW>::t*)(vp + vrow[j] * DV + BASE + n * VW);
+}
+// O^T += V^T . P^T for these channels
+#if POOL == 2
+// (whole numbers moved to 0 .. 255 as for K; `bias`, 128 sum p below zero, is where the sums begin, and `unit` what a probability
+// of the step stands for)
+template <int VW, int T0> DEV void values(f32x4* o, typename vvec<VW>::t (&x)[8], const pfrag_t (&p)[PN], const f32x4 bias, const float unit) {
+  u32 y[8][(VW + 3) / 4];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (VW == 8) { y[j][0] = x[j][0] ^ 0x80808080u; y[j][1] = x[j][1] ^ 0x80808080u; }
+    else y[j][0] = (u32)x[j] ^ 0x80808080u;
+  }
+#pragma unroll
+  for (int e = 0; e < VW; ++e) {
+    u32x4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(y[2 * i + 1][e / 4], y[2 * i][e / 4], 0x0c040c00u + 0x00010001u * (e % 4));
+    f32x4 z = bias;
+#pragma unroll
+    for (int i = 0; i < PN; ++i) z = PV_MFMA(__builtin_bit_cast(pfrag_t, a), p[i], z, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[T0 + e][i] = __builtin_fmaf(unit, z[i], o[T0 + e][i]);
+  }
+}
+#else
+template <int VW, int T0> DEV void values(f32x4* o, typename vvec<VW>::t (&x)[8], const u32 seen, const pfrag_t (&p)[PN], const int h) {
   // a masked key's probability is zero, but zero times what its slot happens to hold (an infinity, NaN) need not be
   if (seen != MASK_ALL) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) x[j] = (vec_t)0;
+    for (int j = 0; j < 8; ++j) x[j] = seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? x[j] : (typename vvec<VW>::t)0;
   }
+  typename vvec<VW>::e y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = __builtin_bit_cast(typename vvec<VW>::e, x[j]);
 #pragma unroll
   for (int e = 0; e < VW; ++e) {
 #if POOL == 0
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[T0 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(pick<VW>(x[j], e), p[j], o[T0 + e], 0, 0, 0);
+    for (int j = 0; j < 8; ++j) o[T0 + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[j][e], p[j], o[T0 + e], 0, 0, 0);
 #else
     pfrag_t a;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = POOL == 1 ? __builtin_bit_cast(pelem_t, (u16)pick<VW>(x[j], e)) : (pelem_t)(float)pick<VW>(x[j], e);
+    for (int j = 0; j < 8; ++j) a[j] = __builtin_bit_cast(pelem_t, (u16)y[j][e]);
 #pragma unroll
     for (int i = 0; i < PN; ++i) o[T0 + e] = PV_MFMA(a, p[i], o[T0 + e], 0, 0, 0);
 #endif
   }
 }
+#endif
 
-extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+// what a wavefront reads in one step: 32 keys and their values
+struct tile_t {
+  typename words<KV * (int)sizeof(pool_t)>::t k[2][NC];
+  V_MEMBERS
+#if POOL == 2
+  f32x4 ks[2], vs[2];
+#endif
+  u32 seen;                                                      // bit i: key i takes part
+};
+
+extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
   __shared__ float Ms[4][16], Ls[4][16];
   __shared__ __attribute__((aligned(16))) float Os[4][GQ][DV + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
@@ -253,6 +296,7 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   if (NSPLIT > 1 && s0 >= s1) return;
   const int* __restrict__ row_of = table + (long long)b * TABLE;
 
+  float q_unit = 1.0f, q_bias = 0.0f;                            // (pools of 8 bits)
   // this lane's query (behind the last one: that again, computed and not stored)
   const qin_t* __restrict__ qp = q + ((long long)b * HQ + head * SHARE + min(q0 + n, SHARE - 1)) * DK;
 #if POOL == 0
@@ -265,6 +309,23 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   }
 #else
   qfrag_t rq[NC][KV / 8][QN];
+  float q_scale = 1.0f;
+#if POOL == 2
+  // queries as float16 of 2^14 at most, whatever their type's range: multiplied by a power of two, which the scores take back
+  {
+    u32 top = 0;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < KV; ++e)
+        if (DK % (4 * KV) == 0 || (c * 4 + h) * KV < DK) top = max(top, __builtin_bit_cast(u32, cvt_in(qp[(c * 4 + h) * KV + e])) & 0x7fffffffu);
+    top = max(top, (u32)__shfl_xor((int)top, 16, 64));
+    top = max(top, (u32)__shfl_xor((int)top, 32, 64));
+    const int up = top == 0 || top >= 0x7f800000u ? 0 : 127 + 14 - (int)(top >> 23);
+    q_scale = __builtin_ldexpf(1.0f, min(up, 127));
+    q_unit = __builtin_ldexpf(1.0f, -min(up, 127));
+  }
+#endif
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -272,11 +333,13 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       const int d = (c * 4 + h) * KV + f * 8;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float x = DK % (4 * KV) == 0 || d < DK ? cvt_in(qp[DK % (4 * KV) == 0 || d < DK ? d + e : 0]) : 0.0f;
+        float x = DK % (4 * KV) == 0 || d < DK ? cvt_in(qp[DK % (4 * KV) == 0 || d < DK ? d + e : 0]) * q_scale : 0.0f;
 #pragma unroll
-        for (int i = 0; i < QN; ++i) { rq[c][f][i][e] = to_q(x); x -= (float)rq[c][f][i][e]; }
+        for (int i = 0; i < QN; ++i) { rq[c][f][i][e] = to_q(x); x -= (float)rq[c][f][i][e]; q_bias += (float)rq[c][f][i][e]; }
       }
     }
+  q_bias += __shfl_xor(q_bias, 16, 64);                          // the rows of K lie 128 too high
+  q_bias = -128.0f * (q_bias + __shfl_xor(q_bias, 32, 64));
 #endif
   f32x4 o[DV / 16];
 #pragma unroll
@@ -285,18 +348,15 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
 
   auto page_at = [&](const int step) {
     const int lp = ((begin / 32 + step * 4 + wave) * 32 + (lane & 31)) / SLOTS;
-    return step < s1 && lp < TABLE ? row_of[lp] : -1;
+    const int page = row_of[min(lp, TABLE - 1)];
+    return step < s1 && lp < TABLE ? page : -1;
   };
-  int page_next = page_at(s0);
-  for (int step = s0; step < s1; ++step) {
-    const int k0 = (begin / 32 + step * 4 + wave) * 32, key = k0 + (lane & 31), page = page_next;
-    page_next = page_at(step + 1);
+  auto fetch = [&](tile_t& t, const int step, const int page) {
+    const int key = (begin / 32 + step * 4 + wave) * 32 + (lane & 31);
     const bool there = (u32)page < (u32)PAGES;
-    const int row = there ? (page * HEADS + head) * SLOTS + key % SLOTS : 0;      // (a page that is not there: row 0, masked)
-    const u32 seen = (u32)__builtin_amdgcn_ballot_w64(there && key >= begin && key < end);
-    if (seen == 0) continue;
-
-    // ---- rows of this lane's keys: as a row of K, and as the eight keys of its scores
+    const int row = there ? (page * HEADS + head) * SLOTS + key % SLOTS : 0;
+    t.seen = (u32)__builtin_amdgcn_ballot_w64(there && key >= begin && key < end);
+    // rows of this lane's keys: as a row of K, and as the eight keys of its scores
     long long krow[2], vrow[8];
     krow[0] = (u32)__shfl(row, n, 64);
     krow[1] = (u32)__shfl(row, 16 + n, 64);
@@ -308,20 +368,25 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) vrow[j] = (u32)__shfl(row, j / 4 * 16 + 4 * h + j % 4, 64);
 #endif
-    kvec_t rk[2][NC];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const int d = (c * 4 + h) * KV;
-        rk[u][c] = *(const kvec_t*)(k_pool + krow[u] * DK + (DK % (4 * KV) == 0 || d < DK ? d : 0));
-        if (DK % (4 * KV) != 0 && d >= DK) rk[u][c] = 0;
+        t.k[u][c] = *(const typename words<KV * (int)sizeof(pool_t)>::t*)(k_pool + krow[u] * DK + (DK % (4 * KV) == 0 || d < DK ? d : 0));
       }
-#if POOL == 2
-    float ks[8], vs[8];
+#if POOL == 2 && SLOTS % 4 == 0
+    t.ks[0] = *(const f32x4*)(k_scale + g0); t.ks[1] = *(const f32x4*)(k_scale + g1);
+    t.vs[0] = *(const f32x4*)(v_scale + g0); t.vs[1] = *(const f32x4*)(v_scale + g1);
+#elif POOL == 2
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { ks[j] = k_scale[vrow[j]]; vs[j] = v_scale[vrow[j]]; }
+    for (int j = 0; j < 8; ++j) { t.ks[j / 4][j % 4] = k_scale[vrow[j]]; t.vs[j / 4][j % 4] = v_scale[vrow[j]]; }
 #endif
+    LOAD_VALUES
+  };
+  auto attend = [&](tile_t& t) {
+    const u32 seen = t.seen;
+    if (seen == 0) return;
     // ---- scores: element i of tile u is key 16 u + 4 h + i of query n
     float s[8];
 #pragma unroll
@@ -329,28 +394,40 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       f32x4 acc = 0.0f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-#if POOL == 0
+        if (DK % (4 * KV) != 0 && (c * 4 + h) * KV >= DK) t.k[u][c] = 0;
+        const krow_t kr = __builtin_bit_cast(krow_t, t.k[u][c]);
+#if POOL == 2
+        // whole numbers as they lie, moved to 0 .. 255: the low bits of a float16, n 2^-24 (the matrix units keep such numbers)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(rk[u][c][e], rq[c][e], acc, 0, 0, 0);
+        for (int f = 0; f < KV / 8; ++f) {
+          const u32 lo = t.k[u][c][f * 2] ^ 0x80808080u, hi = t.k[u][c][f * 2 + 1] ^ 0x80808080u;
+          const u32x4 a = {__builtin_amdgcn_perm(0u, lo, 0x0c010c00u), __builtin_amdgcn_perm(0u, lo, 0x0c030c02u),
+                           __builtin_amdgcn_perm(0u, hi, 0x0c010c00u), __builtin_amdgcn_perm(0u, hi, 0x0c030c02u)};
+#pragma unroll
+          for (int i = 0; i < QN; ++i) acc = QK_MFMA(__builtin_bit_cast(qfrag_t, a), rq[c][f][i], acc, 0, 0, 0);
+        }
+#elif POOL == 0
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[e], rq[c][e], acc, 0, 0, 0);
 #else
 #pragma unroll
         for (int f = 0; f < KV / 8; ++f) {
           qfrag_t a;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = POOL == 1 ? __builtin_bit_cast(qelem_t, (u16)rk[u][c][f * 8 + e]) : to_q((float)rk[u][c][f * 8 + e]);
+          for (int e = 0; e < 8; ++e) a[e] = __builtin_bit_cast(qelem_t, (u16)kr[f * 8 + e]);
 #pragma unroll
           for (int i = 0; i < QN; ++i) acc = QK_MFMA(a, rq[c][f][i], acc, 0, 0, 0);
         }
 #endif
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[u * 4 + i] = acc[i] * SCALE;
+      for (int i = 0; i < 4; ++i) s[u * 4 + i] = POOL == 2 ? __builtin_fmaf(acc[i], 16777216.0f, q_bias) * SCALE * q_unit : acc[i] * SCALE;
     }
     float mx = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
 #if POOL == 2
-      s[j] *= ks[j];
+      s[j] *= t.ks[j / 4][j % 4];
 #endif
       if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) s[j] = -__builtin_inff();
       mx = fmaxf(mx, s[j]);
@@ -367,18 +444,27 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       m_run = m_next;
       l_run *= alpha;
 #pragma unroll
-      for (int t = 0; t < DV / 16; ++t)
+      for (int i = 0; i < DV / 16; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[t][i] *= alpha;
+        for (int e = 0; e < 4; ++e) o[i][e] *= alpha;
     }
     const float m2 = m_run == -__builtin_inff() ? 0.0f : m_run;
+#if POOL == 2
+    // a value's step goes to its probability, relative to the largest step of these keys (float16 has the range for nothing else)
+    float unit = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) unit = fmaxf(unit, seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? t.vs[j / 4][j % 4] : 0.0f);
+    unit = fmaxf(unit, __shfl_xor(unit, 16, 64));
+    unit = fmaxf(unit, __shfl_xor(unit, 32, 64));
+    const float per_unit = unit > 0.0f ? dn_rcp(unit) : 0.0f;
+#endif
     pfrag_t p[PN];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       float x = dn_exp2(s[j] - m2);
       l_run += x;                                                // the sum keeps fp32
 #if POOL == 2
-      x = seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? x * vs[j] : 0.0f;
+      x = seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? x * 128.0f * (t.vs[j / 4][j % 4] * per_unit) : 0.0f;
 #endif
 #if POOL == 0
       p[j] = x;
@@ -387,7 +473,44 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       for (int i = 0; i < PN; ++i) { p[i][j] = (pelem_t)x; x -= (float)p[i][j]; }
 #endif
     }
+#if POOL == 2
+    f32x4 bias = 0.0f;
+    pfrag_t ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = (pelem_t)(-128.0f * 5.9604644775390625e-8f);
+#pragma unroll
+    for (int i = 0; i < PN; ++i) bias = PV_MFMA(ones, p[i], bias, 0, 0, 0);
+#endif
     VALUES
+  };
+  int page = page_at(s0);
+  tile_t t0;
+#if AHEAD
+  if (s1 - s0 > 1) {
+    // The next step's rows are on their way while this one's are worked on, their page numbers one step before that: all
+    // wavefronts begin together, and without it they would all wait together and then all compute.  (The last step is
+    // fetched once more at the end, from the caches, rather than not at all: loads behind a branch make the next wait one for
+    // all of them.)
+    tile_t t1;
+    int page1 = page_at(s0 + 1);
+    fetch(t0, s0, page);
+    page = page_at(min(s0 + 2, s1 - 1));
+    for (int step = s0; step < s1; step += 2) {
+      fetch(t1, min(step + 1, s1 - 1), page1);
+      page1 = page_at(min(step + 3, s1 - 1));
+      __builtin_amdgcn_sched_barrier(0);
+      attend(t0);
+      fetch(t0, min(step + 2, s1 - 1), page);
+      page = page_at(min(step + 4, s1 - 1));
+      __builtin_amdgcn_sched_barrier(0);
+      if (step + 1 < s1) attend(t1);
+    }
+  } else
+#endif
+  for (int step = s0; step < s1; ++step) {
+    fetch(t0, step, page);
+    page = page_at(step + 1);
+    attend(t0);
   }
 
   // ---- the workgroup's four wavefronts joined
@@ -409,6 +532,7 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       l += a * Ls[w][r];
       x += a * Os[w][r][d];
     }
+    if (POOL == 2) x *= 131072.0f;                              // sums were in numbers of 2^-24 and probabilities of 128
     const long long at = (long long)b * HQ + head * SHARE + q0 + r;
 #if NSPLIT > 1
     scratch[PART_AT + (at * NSPLIT + split) * DV + d] = x;
@@ -422,10 +546,11 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
 }
 )KRN";
 
-// Joins the splits of one query: weights 2^(m_s - m) / l, l = sum_s 2^(m_s - m) l_s; a workgroup's threads are DV channels wide and
-// share the splits among the rest.
+// Joins the splits of one query: weights 2^(m_s - m) / l, l = sum_s 2^(m_s - m) l_s.  The threads are DV / 4 vectors wide and share the
+// splits among the rest.
 const char* kJoinBody = R"KRN(
-#define ROWS (256 / DV > 0 ? 256 / DV : 1)
+#define WIDE (DV / 4)
+#define ROWS (256 / WIDE)
 DEV void span_of(const int b, const int* __restrict__ held, int& splits) {
   const int end = min(max(held[b], 0), TABLE * SLOTS), begin = WINDOW > 0 ? max(0, end - WINDOW) : 0;
   const int tiles = (end + 31) / 32 - begin / 32, steps = end > begin ? (tiles + 3) / 4 : 0;
@@ -433,42 +558,58 @@ DEV void span_of(const int b, const int* __restrict__ held, int& splits) {
   splits = (steps + per - 1) / per;
 }
 extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
-  __shared__ float w[NSPLIT], part[ROWS][DV];
-  const int tid = threadIdx.x;
+  __shared__ float w[NSPLIT], inv;
+  __shared__ f32x4 part[ROWS][WIDE];
+  const int tid = threadIdx.x, r = tid / WIDE, d = tid % WIDE;
   const long long at = blockIdx.x;
   int splits;
   span_of((int)(at / HQ), held, splits);
+  // the sums of the first splits are on their way while the weights are found
+  const f32x4* __restrict__ p = (const f32x4*)(scratch + PART_AT + at * NSPLIT * DV) + d;
+  f32x4 x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = 0.0f; if (r < ROWS && r + i * ROWS < splits) x[i] = p[(r + i * ROWS) * WIDE]; }
   const float* __restrict__ ml = scratch + at * NSPLIT * 2;
   if (tid < 64) {
-    float m = -__builtin_inff();
-    for (int s = tid; s < splits; s += 64) m = fmaxf(m, ml[s * 2]);
+    float m = -__builtin_inff(), ms[2], ls[2];                   // (at most 128 splits)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool on = tid + i * 64 < splits;
+      ms[i] = on ? ml[(tid + i * 64) * 2] : -__builtin_inff();
+      ls[i] = on ? ml[(tid + i * 64) * 2 + 1] : 0.0f;
+      m = fmaxf(m, ms[i]);
+    }
     m = dn_wave_max(m);
     float l = 0.0f;
-    for (int s = tid; s < splits; s += 64) {
-      const float a = m == -__builtin_inff() ? 0.0f : dn_exp2(ml[s * 2] - m);
-      w[s] = a;
-      l += a * ml[s * 2 + 1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float a = m == -__builtin_inff() ? 0.0f : dn_exp2(ms[i] - m);
+      if (tid + i * 64 < splits) { w[tid + i * 64] = a; l += a * ls[i]; }
     }
     l = dn_wave_sum(l);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    for (int s = tid; s < splits; s += 64) w[s] = inv == 0.0f && l == 0.0f ? 0.0f : w[s] * inv;
+    if (tid == 0) inv = l == 0.0f ? 0.0f : 1.0f / l;             // (no key, or all of them at -infinity: zeros)
   }
   __syncthreads();
-  const int d = tid % DV, r = tid / DV;
   if (r < ROWS) {
-    float x = 0.0f;
-    const float* __restrict__ p = scratch + PART_AT + at * NSPLIT * DV + d;
-    for (int s = r; s < splits; s += ROWS) x += w[s] * p[(long long)s * DV];
-    part[r][d] = x;
+    f32x4 y = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (r + i * ROWS < splits) y += x[i] * w[r + i * ROWS];
+    for (int s = r + 4 * ROWS; s < splits; s += 4 * ROWS) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[i] = 0.0f; if (s + i * ROWS < splits) x[i] = p[(s + i * ROWS) * WIDE]; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) if (s + i * ROWS < splits) y += x[i] * w[s + i * ROWS];
+    }
+    part[r][d] = y;
   }
   __syncthreads();
   if (tid < DV) {
-    float x = 0.0f;
+    float y = 0.0f;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) x += part[i][tid];
-    qin_t y;
-    cvt_out(&y, x);
-    out[at * DV + tid] = y;
+    for (int i = 0; i < ROWS; ++i) y += ((const float*)part[i])[tid];
+    qin_t e;
+    cvt_out(&e, y * inv);
+    out[at * DV + tid] = e;
   }
 }
 )KRN";
@@ -557,11 +698,20 @@ Lowered lower_cache(LowerCtx& c) {
   const int64_t share = o.HQ / o.HK, qtiles = (share + 15) / 16;
   const int64_t window = op.i("window", 0), most = window > 0 ? std::min(window + 31, o.M * o.S) : o.M * o.S;
   const double scale = op.has("scale") ? op.f("scale", 1) : 1.0 / std::sqrt((double)o.D[0]);
-  // Workgroups for about four per compute unit, and at least one step (128 keys) each at the table's capacity.  Behind
-  // shorter sequences the splits a kernel does not need end at once.
-  const int64_t units = o.B * o.HK * qtiles, steps = (most + 127) / 128;
-  const int64_t nsplit = std::max<int64_t>(1, std::min<int64_t>({steps, (1024 + units - 1) / units, 128}));
   const int form = o.eight_bits ? 2 : dt == DNNF_F32 ? 0 : 1;
+  const int qn = form == 2 && dt == DNNF_F32 ? 3 : 1, pn = form == 0 ? 8 : dt == DNNF_F32 ? 3 : 2;
+  // A step's rows take (channels of a key + channels of a value) / 8 registers for every byte of their type, beside queries, sums
+  // and the work in between; a SIMD unit has 512 for its wavefronts.  Two steps of rows where that leaves two wavefronts.
+  const int64_t rows_regs = (o.D[0] + o.D[1]) * dtype_bytes(stored) / 8 + (form == 2 ? 16 : 0), other = o.D[1] / 4 + o.D[0] / 8 * (form == 0 ? 2 : qn) + 46;
+  const bool ahead = 2 * rows_regs + other <= 256;
+  const int64_t resident = std::max<int64_t>(1, std::min<int64_t>(4, 512 / ((ahead ? 2 : 1) * rows_regs + other)));
+  // As many workgroups as the chip holds at once, with one step (128 keys) each at least at the table's capacity.  Pools of 8 bits,
+  // 64 sequences of 2048, eight key heads of 128 channels: 57 us with two workgroups per compute unit, 65 with three or four (a
+  // second, partly filled round); two sequences of 32768 in bfloat16 53 and 58 us.  Splits that shorter sequences do not need
+  // end at once.
+  const int64_t units = o.B * o.HK * qtiles, steps = (most + 127) / 128;
+  const int64_t nsplit = std::max<int64_t>(1, std::min<int64_t>({steps, (256 * resident + units - 1) / units, 128}));
+  k << "#define AHEAD " << (int)ahead << "\n#define OCCUPANCY " << resident << "\n";
   char num[40];
   snprintf(num, sizeof num, "%.9gf", scale * 1.4426950408889634);
   std::string sc = num;
@@ -569,22 +719,24 @@ Lowered lower_cache(LowerCtx& c) {
   const int64_t rows = o.B * o.HQ, part_at = (rows * nsplit * 2 + 3) / 4 * 4;
   k << "typedef " << c.ctype(dt) << " qin_t;\n#define POOL " << form << "\n#define HQ " << o.HQ << "\n#define WINDOW " << window << "\n#define NSPLIT " << nsplit
     << "\n#define QTILES " << qtiles << "\n#define GQ " << std::min<int64_t>(share, 16) << "\n#define SCALE " << sc << "\n#define PART_AT " << part_at << "\n";
-  // Types of the products' operands.  Pools of 16 bits: queries and rows as they are.  Pools of 8 bits: rows are whole numbers up
-  // to 127, exact in either type; a value's step goes to its probability, whose range only bfloat16 has.  Probabilities are
-  // given in two parts (three for fp32 results): rounded once to 8 bits they would add as much error as the rounding of the
-  // result (1.4 times its error in all), and the matrix units have time for the second part.
-  const std::string h16 = dt == DNNF_F16 ? "_Float16" : "__bf16", mf = "__builtin_amdgcn_mfma_f32_16x16x32_";
-  const int qn = form == 2 && dt == DNNF_F32 ? 3 : 1, pn = form == 0 ? 8 : dt == DNNF_F32 ? 3 : 2;
-  k << "typedef " << (form == 0 ? "float" : h16) << " qelem_t;\ntypedef " << (form == 0 ? "float" : form == 1 ? h16 : "__bf16") << " pelem_t;\n#define QN " << qn << "\n#define PN " << pn
-    << "\n#define QK_MFMA " << mf << (dt == DNNF_F16 ? "f16" : "bf16") << "\n#define PV_MFMA " << mf << (form == 1 && dt == DNNF_F16 ? "f16" : "bf16") << "\n";
+  // Types of the products' operands.  Pools of 16 bits: queries and rows as they are.  Pools of 8 bits: float16, which holds the
+  // rows' bytes without any arithmetic.  Probabilities are given in two parts (three for fp32 results): rounded once to
+  // 8 bits they would add as much error as the rounding of the result (1.4 times its error in all), and the matrix units have
+  // time for the second part.
+  const std::string h16 = form == 2 || dt == DNNF_F16 ? "_Float16" : "__bf16", mf = std::string("__builtin_amdgcn_mfma_f32_16x16x32_") + (form == 2 || dt == DNNF_F16 ? "f16" : "bf16");
+  k << "typedef " << (form == 0 ? "float" : h16) << " qelem_t;\ntypedef " << (form == 0 ? "float" : h16) << " pelem_t;\n#define QN " << qn << "\n#define PN " << pn
+    << "\n#define QK_MFMA " << mf << "\n#define PV_MFMA " << mf << "\n";
   // a value's channels in runs of 128, 64, 32 and 16: 8, 4, 2 or 1 for each of the sixteen lanes of a quarter (fp32: 64 at most,
   // 16-byte loads)
-  std::string values, to_lds;
+  std::string members, loads, values, to_lds;
   int tile = 0;
   for (int64_t at = 0; at < o.D[1];) {
     int64_t w = form == 0 ? 4 : 8;
     while (w * 16 > o.D[1] - at) w /= 2;
-    values += "    values<" + std::to_string(at) + ", " + std::to_string(w) + ", " + std::to_string(tile) + ">(o, v_pool, vrow, seen, p, n, h); \\\n";
+    const std::string W = std::to_string(w), v = "v" + std::to_string(at);
+    members += "  vvec<" + W + ">::t " + v + "[8]; \\\n";
+    loads += "    load_values<" + std::to_string(at) + ", " + W + ">(t." + v + ", v_pool, vrow, n); \\\n";
+    values += "    values<" + W + ", " + std::to_string(tile) + ">(o, t." + v + (form == 2 ? ", p, bias, unit); \\\n" : ", seen, p, h); \\\n");
     for (int64_t e = 0; e < w; e++)
       for (int i = 0; i < 4; i++)
         to_lds += "    Os[wave][n][" + std::to_string(at + e + i * w) + " + h * " + std::to_string(4 * w) + "] = o[" + std::to_string(tile + e) + "][" + std::to_string(i) + "]; \\\n";
@@ -595,7 +747,7 @@ Lowered lower_cache(LowerCtx& c) {
   params.insert(params.begin(), o.q);
   if (nsplit == 1) params.push_back(op.out[0]);
   const std::string main_params = "#define KPARAMS const qin_t* __restrict__ q, " + pools + (nsplit > 1 ? ", float* __restrict__ scratch" : ", qin_t* __restrict__ out") + "\n";
-  L.launches.push_back(make_launch("dnnf_cache_attend", head + main_params + "#define VALUES \\\n" + values + "\n#define OUT_TO_LDS \\\n" + to_lds + "\n", kAttendBody, params, units * nsplit));
+  L.launches.push_back(make_launch("dnnf_cache_attend", head + main_params + "#define V_MEMBERS \\\n" + members + "\n#define LOAD_VALUES \\\n" + loads + "\n#define VALUES \\\n" + values + "\n#define OUT_TO_LDS \\\n" + to_lds + "\n", kAttendBody, params, units * nsplit));
   if (nsplit > 1) {
     L.launches[0].scratch = true;
     L.scratch_bytes = (part_at + rows * nsplit * o.D[1]) * 4;

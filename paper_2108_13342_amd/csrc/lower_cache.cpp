@@ -46,25 +46,58 @@ DEV int written_page(const int e, const int* __restrict__ table, const int* __re
   return p0 < hi ? table[(long long)b * TABLE + lp] : -1;
 }
 
-template <int D> DEV void put(pool_t* __restrict__ pool, float* __restrict__ scale, const elem_t* __restrict__ x, const long long src, const long long dst, const int lane) {
-  const bool on = lane < VECTORS(D);
+template <int D> DEV in_t take(const elem_t* __restrict__ x, const long long src, const int lane) {
   in_t v = 0;
-  if (on) v = *(const in_t*)(x + src * D + lane * VEC);
+  if (VECTORS(D) == LANES || lane < VECTORS(D)) v = *(const in_t*)(x + src * D + lane * VEC);
+  return v;
+}
+template <int D> DEV void put(pool_t* __restrict__ pool, float* __restrict__ scale, const in_t v, const long long dst, const int lane) {
+  const bool on = VECTORS(D) == LANES || lane < VECTORS(D);
 #if EIGHT_BITS
   float f[VEC];
-  u32 top = 0;                                     // the largest magnitude, by bits: infinities and NaN lie above all others
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) { f[e] = cvt_in(v[e]); top = max(top, __builtin_bit_cast(u32, f[e]) & 0x7fffffffu); }
+  for (int e = 0; e < VEC; ++e) f[e] = cvt_in(v[e]);
+  // the largest magnitude, by bits: infinities and NaN lie above all others
+#if ELEM_BYTES == 2
+  const u16x8 m = __builtin_bit_cast(u16x8, v) & (u16)0x7fff;
+  const u16x4 m4 = __builtin_elementwise_max((u16x4){m[0], m[1], m[2], m[3]}, (u16x4){m[4], m[5], m[6], m[7]});
+  const u16x2 m2 = __builtin_elementwise_max((u16x2){m4[0], m4[1]}, (u16x2){m4[2], m4[3]});
+  u32 top = max((u32)m2[0], (u32)m2[1]);
+#else
+  u32 top = 0;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) top = max(top, __builtin_bit_cast(u32, f[e]) & 0x7fffffffu);
+#endif
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, (u32)__shfl_xor((int)top, o, 64));
+#if ELEM_BYTES == 2
+  top = __builtin_bit_cast(u32, cvt_in(__builtin_bit_cast(elem_t, (u16)top)));
+#endif
   // a row with an infinity or NaN reads back as NaN; one that lies wholly below 2^-119 (where the step would leave the
   // normal numbers) as zeros
   float step = __builtin_bit_cast(float, top) / 127.0f;
   if (top < 0x04000000u) step = 0.0f;
   if (top >= 0x7f800000u) step = __builtin_nanf("");
   out_t q;
+  if (__builtin_amdgcn_ballot_w64(!(step >= 7.9e-31f)) != 0) {     // (rows of zeros, tiny ones, infinities and NaN)
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) q[e] = (pool_t)(step > 0.0f ? __builtin_rintf(f[e] / step) : 0.0f);
+    for (int e = 0; e < VEC; ++e) q[e] = (pool_t)(step > 0.0f ? __builtin_rintf(f[e] / step) : 0.0f);
+  } else {
+    // the correctly rounded quotient all the same: from the correctly rounded reciprocal, one correction by the exact
+    // remainder is enough (Markstein) where that is a normal number
+    const float inv = 1.0f / step;
+    u32 n[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float y = f[e] * inv, z = __builtin_fmaf(__builtin_fmaf(-y, step, f[e]), inv, y);
+      n[e] = __builtin_bit_cast(u32, z + 12582912.0f);          // (behind 3 * 2^22 a float's low bits are the nearest whole number)
+    }
+    u32 w[VEC / 4];
+#pragma unroll
+    for (int e = 0; e < VEC; e += 4)
+      w[e / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(n[e + 3], n[e + 2], 0x0c0c0400u), __builtin_amdgcn_perm(n[e + 1], n[e], 0x0c0c0400u), 0x05040100u);
+    __builtin_memcpy(&q, w, sizeof q);
+  }
   if (on) *(out_t*)(pool + dst * D + lane * VEC) = q;
   if (lane == 0) scale[dst] = step;
 #else
@@ -72,12 +105,12 @@ template <int D> DEV void put(pool_t* __restrict__ pool, float* __restrict__ sca
 #endif
 }
 
-// A workgroup writes CHUNK positions that lie in one page, for every head; LANES lanes a row.  Where one slot is written
+// A workgroup writes CHUNK positions that lie in one page, for HEADS_EACH heads; LANES lanes a row.  Where one slot is written
 // twice in a call the last write stays (sequences in order, then tokens): a workgroup looks through the written pages behind
 // its own for the same page - once, and row by row only if there is one.
 extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   __shared__ int clash;
-  const int tid = threadIdx.x, unit = blockIdx.x;
+  const int tid = threadIdx.x, unit = blockIdx.x, head0 = blockIdx.y * HEADS_EACH;
   const int entry = unit / SUBS, b = entry / SPANS;
   int f, lo, hi;
   written(b, first, count, f, lo, hi);
@@ -89,6 +122,16 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   const int page = table[(long long)b * TABLE + lp];
   if ((u32)page >= (u32)PAGES) return;
   if (tid == 0) clash = 0;
+  // the rows are on their way while the other pages are looked through
+  const int lane = tid % LANES, rows = (p1 - p0) * HEADS_EACH;
+  in_t kx[PASSES], vx[PASSES];
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const int r = min(tid / LANES + i * (256 / LANES), rows - 1), h = min(head0 + r % HEADS_EACH, HEADS - 1);
+    const long long src = ((long long)b * TOKENS + (p0 + r / HEADS_EACH - f)) * HEADS + h;
+    kx[i] = take<DK>(k, src, lane);
+    vx[i] = take<DV>(v, src, lane);
+  }
   __syncthreads();
   bool same = false;
   for (int e = entry + 1 + tid; e < SEQUENCES * SPANS; e += 256) {
@@ -97,9 +140,10 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   }
   if (same) clash = 1;
   __syncthreads();
-  const int lane = tid % LANES;
-  for (int r = tid / LANES; r < (p1 - p0) * HEADS; r += 256 / LANES) {
-    const int p = p0 + r / HEADS, h = r % HEADS;
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const int r = tid / LANES + i * (256 / LANES), p = p0 + r / HEADS_EACH, h = head0 + r % HEADS_EACH;
+    if (r >= rows || h >= HEADS) continue;
     if (clash) {
       bool later = false;
       for (int e = entry + 1; e < SEQUENCES * SPANS && !later; ++e) {
@@ -108,9 +152,9 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
       }
       if (later) continue;
     }
-    const long long src = ((long long)b * TOKENS + (p - f)) * HEADS + h, dst = ((long long)page * HEADS + h) * SLOTS + p % SLOTS;
-    put<DK>(k_pool, k_scale, k, src, dst, lane);
-    put<DV>(v_pool, v_scale, v, src, dst, lane);
+    const long long dst = ((long long)page * HEADS + h) * SLOTS + p % SLOTS;
+    put<DK>(k_pool, k_scale, kx[i], dst, lane);
+    put<DV>(v_pool, v_scale, vx[i], dst, lane);
   }
 }
 )KRN";
@@ -660,9 +704,14 @@ Lowered lower_cache(LowerCtx& c) {
     const int64_t spans = (o.T + o.S - 2) / o.S + 1, subs = (o.S + chunk - 1) / chunk;
     int64_t lanes = 1;
     while (lanes * vec < std::max(o.D[0], o.D[1])) lanes *= 2;
+    // rows a lane: four where that leaves two workgroups per compute unit, else two or one (4 x 1024 tokens of twelve heads of 64
+    // channels: 3.9 us; 7.6 with all heads of sixteen tokens in a workgroup)
+    const int64_t at_once = 256 / lanes, tokens = std::min(chunk, o.T), passes_of = o.B * o.T * o.HK / at_once;
+    const int64_t want = passes_of >= 4 * 512 ? 4 : passes_of >= 2 * 512 ? 2 : 1;
+    const int64_t heads = std::min(o.HK, std::max<int64_t>(1, want * at_once / tokens)), passes = (tokens * heads + at_once - 1) / at_once;
     DNNF_CHECK(o.B * spans < (int64_t)1 << 30, DNNF_UNSUPPORTED_OP, "CacheWrite: too many pages in one call");
-    k << "typedef " << elem << " elem_t;\n#define TOKENS " << o.T << "\n#define SPANS " << spans << "\n#define SUBS " << subs << "\n#define CHUNK " << chunk
-      << "\n#define LANES " << lanes << "\n#define HAS_COUNT " << (int)(o.count >= 0) << "\n";
+    k << "typedef " << elem << " elem_t;\n#define ELEM_BYTES " << 16 / vec << "\n#define TOKENS " << o.T << "\n#define SPANS " << spans << "\n#define SUBS " << subs << "\n#define CHUNK " << chunk
+      << "\n#define LANES " << lanes << "\n#define HEADS_EACH " << heads << "\n#define PASSES " << passes << "\n#define HAS_COUNT " << (int)(o.count >= 0) << "\n";
     if (o.count < 0) k << "#define count ((const int*)0)\n";
     k << "#define KPARAMS pool_t* __restrict__ k_pool, pool_t* __restrict__ v_pool" << scales(true) << ", const elem_t* __restrict__ k, const elem_t* __restrict__ v, "
       << "const int* __restrict__ table, const int* __restrict__ first" << (o.count >= 0 ? ", const int* __restrict__ count" : "") << "\n";
@@ -671,6 +720,8 @@ Lowered lower_cache(LowerCtx& c) {
     if (o.count >= 0) params.push_back(o.count);
     for (size_t i = 0; i < op.out.size(); i++) L.in_place.push_back({op.out[i], op.in[i]});
     L.launches.push_back(make_launch("dnnf_cache_write", k.str(), kWriteBody, params, o.B * spans * subs));
+    L.launches[0].grid[1] = (unsigned)((o.HK + heads - 1) / heads);
+    DNNF_CHECK(L.launches[0].grid[1] < 65536, DNNF_UNSUPPORTED_OP, "CacheWrite: too many heads");
     L.variant = "cache_write_chunk" + std::to_string(chunk) + (o.eight_bits ? "_i8" : "");
     return L;
   }

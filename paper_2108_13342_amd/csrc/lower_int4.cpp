@@ -84,6 +84,10 @@ DEV frag_t decode(const u32 w) {
 
 extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   __shared__ __attribute__((aligned(16))) float part[WAVES][ROWS][16 * NT + 1];
+#if STAGED
+  // x once per workgroup in the order of the codes (rows 16 bytes apart in their banks, zeros behind K)
+  __shared__ __attribute__((aligned(16))) part_t xs[XP][ROWS][CHUNKS * CHUNK + 8];
+#endif
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
   const idx_t c0 = (idx_t)blockIdx.x * (16 * NT), r0 = (idx_t)blockIdx.y * (16 * MT);
   const unsigned char* __restrict__ wr[NT];
@@ -98,12 +102,13 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
     zr[t] = PZ + (long long)col * GROUPS;
 #endif
   }
+#if !STAGED
   const elem_t* __restrict__ xr[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) xr[t] = PX + offX_batch(0) + offX_row(min(r0 + t * 16 + n, (idx_t)(GM - 1)));
+#endif
 
   auto load = [&](run_t& r, const int c) {
-    if (c >= CHUNKS) return;
     const int at = c * (CHUNK / 2) + h * 16;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -165,7 +170,12 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           frag_t x[XP];
+#if STAGED
+#pragma unroll
+          for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(t * 16 + n, ROWS - 1)][k];
+#else
           load_x(xr[t], k, x);
+#endif
 #pragma unroll
           for (int q = 0; q < XP; ++q) {
             sx[t] = MFMA(x[q], ones, sx[t], 0, 0, 0);
@@ -180,21 +190,31 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[t][e], sum[t][u][e]), acc[t][u][e]);
+          for (int e = 0; e < (ROWS < 4 ? ROWS : 4); ++e) acc[t][u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[t][e], sum[t][u][e]), acc[t][u][e]);
       }
     }
   };
 
+  // this wavefront's chunks: EACH successive ones, so that it reads runs of EACH * 64 bytes of a row; AHEAD of them on their way
+  const int first = wave * EACH, last = min(first + EACH, CHUNKS);
   run_t ring[AHEAD];
 #pragma unroll
-  for (int p = 0; p < AHEAD; ++p) load(ring[p], wave + p * WAVES);
-  for (int c = wave; c < CHUNKS; c += WAVES * AHEAD) {
+  for (int p = 0; p < AHEAD; ++p) load(ring[p], max(min(first + p, last - 1), 0));
+#if STAGED
+  for (int i = tid; i < ROWS * (CHUNKS * 16); i += 64 * WAVES) {
+    const int r = i / (CHUNKS * 16), k = i % (CHUNKS * 16) * 8;
+    frag_t x[XP];
+    load_x(PX + offX_batch(0) + offX_row(min(r0 + r, (idx_t)(GM - 1))), k, x);
+#pragma unroll
+    for (int q = 0; q < XP; ++q) *(frag_t*)&xs[q][r][k] = x[q];
+  }
+  __syncthreads();
+#endif
+  for (int c = first; c < last; c += AHEAD) {
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
-      const int cc = c + p * WAVES;
-      if (cc >= CHUNKS) break;
-      multiply(ring[p], cc);
-      load(ring[p], cc + WAVES * AHEAD);
+      if (c + p < last) multiply(ring[p], c + p);
+      if (EACH > AHEAD) load(ring[p], min(c + p + AHEAD, last - 1));      // (unconditional: loads behind a branch make the next wait one for all)
     }
   }
 
@@ -286,20 +306,26 @@ Lowered lower_int4(LowerCtx& c) {
   for (int t : params) wide = wide || g.tensors[t].n() >= (int64_t)1 << 31;
   wide = wide || M * N >= (int64_t)1 << 31;
 
-  // ---- tile: all rows up to 64; as many columns as leave two workgroups per compute unit; K split among the wavefronts
+  // ---- tile: all rows up to 64; as many columns as leave two workgroups per compute unit; K split among up to sixteen
+  // wavefronts.  A product of one row is over before a long loop could settle: what counts is that all of its weights are asked
+  // for at once (11008 x 4096, bfloat16, one row: 9.6 us with sixteen wavefronts, 11.7 with eight, 14.3 with four).
   const int64_t MT = std::min<int64_t>(4, (M + 15) / 16), row_tiles = (M + 16 * MT - 1) / (16 * MT), chunks = (K + 127) / 128;
   int64_t NT = 4;
   while (NT > 1 && (N + 16 * NT - 1) / (16 * NT) * row_tiles < 512) NT /= 2;
-  const int64_t waves = std::min<int64_t>(8, chunks), ahead = std::min<int64_t>(2, (chunks + waves - 1) / waves);
+  const int64_t most = std::min<int64_t>(16, chunks), each = (chunks + most - 1) / most, waves = (chunks + each - 1) / each, ahead = std::min<int64_t>(each, 2);
+  // x goes through LDS where that is less work than the weights that a workgroup reads (one row, 4096 x 11008: 10.0 us and 14.3 with
+  // x read by every wavefront for itself; sixteen rows, 50257 x 768: 12.3 and 9.5)
+  const int64_t xp = X.dtype == DNNF_F32 ? 3 : 1, staged_bytes = xp * std::min(M, 16 * MT) * (chunks * 128 + 8) * 2;
+  const bool staged = staged_bytes <= 40 * 1024 && staged_bytes * 10 <= 9 * (16 * NT * K / 2);
   const int steps = G % 128 == 0 || G >= K ? 4 : G % 64 == 0 ? 2 : 1;
 
   std::ostringstream k;
   const std::string part = X.dtype == DNNF_F16 ? "_Float16" : "__bf16";
   k << "typedef " << (wide ? "long long" : "int") << " idx_t;\ntypedef " << c.ctype(X.dtype) << " elem_t;\ntypedef " << part << " part_t;\n";
-  k << "#define ELEM_BYTES " << dtype_bytes(X.dtype) << "\n#define XP " << (X.dtype == DNNF_F32 ? 3 : 1) << "\n#define F16_PARTS " << (int)(X.dtype == DNNF_F16) << "\n";
+  k << "#define ELEM_BYTES " << dtype_bytes(X.dtype) << "\n#define XP " << xp << "\n#define F16_PARTS " << (int)(X.dtype == DNNF_F16) << "\n";
   k << "#define MFMA __builtin_amdgcn_mfma_f32_16x16x32_" << (X.dtype == DNNF_F16 ? "f16" : "bf16") << "\n";
   k << "#define GM " << M << "\n#define GN " << N << "\n#define GK " << K << "\n#define GROUP " << G << "\n#define GROUPS " << groups << "\n#define HAS_ZERO " << (int)has_zero << "\n";
-  k << "#define MT " << MT << "\n#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define STEPS " << steps << "\n";
+  k << "#define MT " << MT << "\n#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define EACH " << each << "\n#define STAGED " << (int)staged << "\n#define STEPS " << steps << "\n";
   k << "#define PX p0\n#define PW p1\n#define PS p2\n#define PZ p3\n";
   k << gemm_offset_fn(c, "offX_row", rows, xa) << gemm_offset_fn(c, "offX_batch", {}, xa);
   const std::string kparams = c.param_list(params, written);

@@ -340,50 +340,12 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
   if (NSPLIT > 1 && s0 >= s1) return;
   const int* __restrict__ row_of = table + (long long)b * TABLE;
 
-  float q_unit = 1.0f, q_bias = 0.0f;                            // (pools of 8 bits)
-  // this lane's query (behind the last one: that again, computed and not stored)
-  const qin_t* __restrict__ qp = q + ((long long)b * HQ + head * SHARE + min(q0 + n, SHARE - 1)) * DK;
+  // this lane's query; filled while the first rows are on their way
+  float q_unit = SCALE, q_bias = 0.0f;                           // (pools of 8 bits: what the scores take back, and the offset of K's rows)
 #if POOL == 0
   float rq[NC][4];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const f32x4 t = *(const f32x4*)(qp + c * 16 + h * 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) rq[c][e] = t[e];
-  }
 #else
   qfrag_t rq[NC][KV / 8][QN];
-  float q_scale = 1.0f;
-#if POOL == 2
-  // queries as float16 of 2^14 at most, whatever their type's range: multiplied by a power of two, which the scores take back
-  {
-    u32 top = 0;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < KV; ++e)
-        if (DK % (4 * KV) == 0 || (c * 4 + h) * KV < DK) top = max(top, __builtin_bit_cast(u32, cvt_in(qp[(c * 4 + h) * KV + e])) & 0x7fffffffu);
-    top = max(top, (u32)__shfl_xor((int)top, 16, 64));
-    top = max(top, (u32)__shfl_xor((int)top, 32, 64));
-    const int up = top == 0 || top >= 0x7f800000u ? 0 : 127 + 14 - (int)(top >> 23);
-    q_scale = __builtin_ldexpf(1.0f, min(up, 127));
-    q_unit = __builtin_ldexpf(1.0f, -min(up, 127));
-  }
-#endif
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int f = 0; f < KV / 8; ++f) {
-      const int d = (c * 4 + h) * KV + f * 8;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float x = DK % (4 * KV) == 0 || d < DK ? cvt_in(qp[DK % (4 * KV) == 0 || d < DK ? d + e : 0]) * q_scale : 0.0f;
-#pragma unroll
-        for (int i = 0; i < QN; ++i) { rq[c][f][i][e] = to_q(x); x -= (float)rq[c][f][i][e]; q_bias += (float)rq[c][f][i][e]; }
-      }
-    }
-  q_bias += __shfl_xor(q_bias, 16, 64);                          // the rows of K lie 128 too high
-  q_bias = -128.0f * (q_bias + __shfl_xor(q_bias, 32, 64));
 #endif
   f32x4 o[DV / 16];
 #pragma unroll
@@ -465,7 +427,7 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
 #endif
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[u * 4 + i] = POOL == 2 ? __builtin_fmaf(acc[i], 16777216.0f, q_bias) * SCALE * q_unit : acc[i] * SCALE;
+      for (int i = 0; i < 4; ++i) s[u * 4 + i] = POOL == 2 ? __builtin_fmaf(acc[i], 16777216.0f, q_bias) * q_unit : acc[i] * SCALE;
     }
     float mx = -__builtin_inff();
 #pragma unroll
@@ -473,9 +435,19 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
 #if POOL == 2
       s[j] *= t.ks[j / 4][j % 4];
 #endif
-      if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) s[j] = -__builtin_inff();
-      mx = fmaxf(mx, s[j]);
     }
+    if (seen != MASK_ALL) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!(seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u)) {
+          s[j] = -__builtin_inff();
+#if POOL == 2
+          t.vs[j / 4][j % 4] = 0.0f;
+#endif
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[j]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     // The reference of the exponentials moves only when a row's maximum has grown by more than 2^8: until then the
@@ -492,12 +464,13 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][e] *= alpha;
     }
-    const float m2 = m_run == -__builtin_inff() ? 0.0f : m_run;
+    // (pools of 8 bits: 2^7 up, towards the middle of float16's range; it cancels in the quotient)
+    const float m2 = (m_run == -__builtin_inff() ? 0.0f : m_run) - (POOL == 2 ? 7.0f : 0.0f);
 #if POOL == 2
     // a value's step goes to its probability, relative to the largest step of these keys (float16 has the range for nothing else)
     float unit = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) unit = fmaxf(unit, seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? t.vs[j / 4][j % 4] : 0.0f);
+    for (int j = 0; j < 8; ++j) unit = fmaxf(unit, t.vs[j / 4][j % 4]);
     unit = fmaxf(unit, __shfl_xor(unit, 16, 64));
     unit = fmaxf(unit, __shfl_xor(unit, 32, 64));
     const float per_unit = unit > 0.0f ? dn_rcp(unit) : 0.0f;
@@ -508,7 +481,7 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
       float x = dn_exp2(s[j] - m2);
       l_run += x;                                                // the sum keeps fp32
 #if POOL == 2
-      x = seen >> (j / 4 * 16 + 4 * h + j % 4) & 1u ? x * 128.0f * (t.vs[j / 4][j % 4] * per_unit) : 0.0f;
+      x *= t.vs[j / 4][j % 4] * per_unit;
 #endif
 #if POOL == 0
       p[j] = x;
@@ -527,8 +500,56 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
 #endif
     VALUES
   };
+  auto query = [&] {
+    // the query (behind the last one: that again, computed and not stored)
+    const qin_t* __restrict__ qp = q + ((long long)b * HQ + head * SHARE + min(q0 + n, SHARE - 1)) * DK;
+#if POOL == 0
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const f32x4 t = *(const f32x4*)(qp + c * 16 + h * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rq[c][e] = t[e];
+    }
+#else
+    float q_scale = 1.0f;
+#if POOL == 2
+    // queries as float16 of 2^14 at most, whatever their type's range: multiplied by a power of two, which the scores take back
+    {
+      u32 top = 0;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < KV; ++e)
+          if (DK % (4 * KV) == 0 || (c * 4 + h) * KV < DK) top = max(top, __builtin_bit_cast(u32, cvt_in(qp[(c * 4 + h) * KV + e])) & 0x7fffffffu);
+      top = max(top, (u32)__shfl_xor((int)top, 16, 64));
+      top = max(top, (u32)__shfl_xor((int)top, 32, 64));
+      const int up = top == 0 || top >= 0x7f800000u ? 0 : 127 + 14 - (int)(top >> 23);
+      q_scale = __builtin_ldexpf(1.0f, min(up, 127));
+      q_unit = __builtin_ldexpf(SCALE, -min(up, 127));
+    }
+#endif
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int f = 0; f < KV / 8; ++f) {
+        const int d = (c * 4 + h) * KV + f * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float x = DK % (4 * KV) == 0 || d < DK ? cvt_in(qp[DK % (4 * KV) == 0 || d < DK ? d + e : 0]) * q_scale : 0.0f;
+#pragma unroll
+          for (int i = 0; i < QN; ++i) { rq[c][f][i][e] = to_q(x); x -= (float)rq[c][f][i][e]; q_bias += (float)rq[c][f][i][e]; }
+        }
+      }
+    q_bias += __shfl_xor(q_bias, 16, 64);                          // the rows of K lie 128 too high
+    q_bias = -128.0f * (q_bias + __shfl_xor(q_bias, 32, 64));
+#endif
+  };
   int page = page_at(s0);
   tile_t t0;
+  fetch(t0, s0, page);
+  page = page_at(max(min(s0 + 2, s1 - 1), s0));
+  int page1 = page_at(s0 + 1);
+  query();
 #if AHEAD
   if (s1 - s0 > 1) {
     // The next step's rows are on their way while this one's are worked on, their page numbers one step before that: all
@@ -536,9 +557,6 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
     // fetched once more at the end, from the caches, rather than not at all: loads behind a branch make the next wait one for
     // all of them.)
     tile_t t1;
-    int page1 = page_at(s0 + 1);
-    fetch(t0, s0, page);
-    page = page_at(min(s0 + 2, s1 - 1));
     for (int step = s0; step < s1; step += 2) {
       fetch(t1, min(step + 1, s1 - 1), page1);
       page1 = page_at(min(step + 3, s1 - 1));
@@ -549,13 +567,15 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
       __builtin_amdgcn_sched_barrier(0);
       if (step + 1 < s1) attend(t1);
     }
-  } else
-#endif
-  for (int step = s0; step < s1; ++step) {
-    fetch(t0, step, page);
-    page = page_at(step + 1);
+  } else if (s0 < s1) attend(t0);
+#else
+  for (int step = s0; step < s1;) {
     attend(t0);
+    if (++step == s1) break;
+    fetch(t0, step, page1);
+    page1 = page_at(step + 1);
   }
+#endif
 
   // ---- the workgroup's four wavefronts joined
   l_run += __shfl_xor(l_run, 16, 64);
@@ -576,7 +596,7 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
       l += a * Ls[w][r];
       x += a * Os[w][r][d];
     }
-    if (POOL == 2) x *= 131072.0f;                              // sums were in numbers of 2^-24 and probabilities of 128
+    if (POOL == 2) x *= 16777216.0f;                            // (the rows were in numbers of 2^-24)
     const long long at = (long long)b * HQ + head * SHARE + q0 + r;
 #if NSPLIT > 1
     scratch[PART_AT + (at * NSPLIT + split) * DV + d] = x;
@@ -606,21 +626,24 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   __shared__ f32x4 part[ROWS][WIDE];
   const int tid = threadIdx.x, r = tid / WIDE, d = tid % WIDE;
   const long long at = blockIdx.x;
-  int splits;
-  span_of((int)(at / HQ), held, splits);
-  // the sums of the first splits are on their way while the weights are found
+  // everything is asked for before it is known how many splits there are (what the others' places hold is not used)
   const f32x4* __restrict__ p = (const f32x4*)(scratch + PART_AT + at * NSPLIT * DV) + d;
   f32x4 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[i] = 0.0f; if (r < ROWS && r + i * ROWS < splits) x[i] = p[(r + i * ROWS) * WIDE]; }
-  const float* __restrict__ ml = scratch + at * NSPLIT * 2;
+  for (int i = 0; i < 4; ++i) { x[i] = 0.0f; if (r < ROWS && r + i * ROWS < NSPLIT) x[i] = p[(r + i * ROWS) * WIDE]; }
+  const f32x2* __restrict__ ml = (const f32x2*)(scratch + at * NSPLIT * 2);
+  f32x2 both[2];                                                 // (at most 128 splits)
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { both[i] = 0.0f; if (tid < 64 && tid + i * 64 < NSPLIT) both[i] = ml[tid + i * 64]; }
+  int splits;
+  span_of((int)(at / HQ), held, splits);
   if (tid < 64) {
-    float m = -__builtin_inff(), ms[2], ls[2];                   // (at most 128 splits)
+    float m = -__builtin_inff(), ms[2], ls[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const bool on = tid + i * 64 < splits;
-      ms[i] = on ? ml[(tid + i * 64) * 2] : -__builtin_inff();
-      ls[i] = on ? ml[(tid + i * 64) * 2 + 1] : 0.0f;
+      ms[i] = on ? both[i][0] : -__builtin_inff();
+      ls[i] = on ? both[i][1] : 0.0f;
       m = fmaxf(m, ms[i]);
     }
     m = dn_wave_max(m);

@@ -28,22 +28,18 @@ const char* kWriteBody = R"KRN(
 typedef elem_t in_t __attribute__((ext_vector_type(VEC)));
 typedef pool_t out_t __attribute__((ext_vector_type(VEC)));
 
-// positions [lo, hi) that sequence b writes
-DEV void written(const int b, const int* __restrict__ first, const int* __restrict__ fresh, int& f, int& lo, int& hi) {
-  f = first[b];
-  const int n = HAS_COUNT ? min(max(fresh[b], 0), TOKENS) : TOKENS;
-  lo = max(f, 0);
-  hi = (int)min((long long)f + n, (long long)TABLE * SLOTS);
+// positions [lo, hi) that a sequence writes whose operands are `f` and `n`
+DEV void written(const int f, const int n, int& lo, int& hi) {
+  lo = min(max(f, 0), TABLE * SLOTS);
+  hi = (int)min((long long)f + min(max(n, 0), TOKENS), (long long)TABLE * SLOTS);
 }
-// the page that entry e of all sequences' written pages lies in; -1: nothing is written there
-DEV int written_page(const int e, const int* __restrict__ table, const int* __restrict__ first, const int* __restrict__ fresh, int& lo, int& hi, int& p0) {
-  const int b = e / SPANS;
-  int f;
-  written(b, first, fresh, f, lo, hi);
-  if (lo >= hi) return -1;
-  const int lp = lo / SLOTS + e % SPANS;
+// the page that entry e of all sequences' written pages lies in, whose first position is p0; -1: nothing is written there
+DEV int written_page(const int e, const int f, const int n, const int* __restrict__ table, int& lo, int& hi, int& p0) {
+  written(f, n, lo, hi);
+  const int lp = min(lo / SLOTS + e % SPANS, TABLE - 1);
+  const int page = table[(long long)(e / SPANS) * TABLE + lp];
   p0 = lp * SLOTS;
-  return p0 < hi ? table[(long long)b * TABLE + lp] : -1;
+  return lo < hi && p0 < hi && lp == lo / SLOTS + e % SPANS ? page : -1;
 }
 
 template <int D> DEV in_t take(const elem_t* __restrict__ x, const long long src, const int lane) {
@@ -112,17 +108,17 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   __shared__ int clash;
   const int tid = threadIdx.x, unit = blockIdx.x, head0 = blockIdx.y * HEADS_EACH;
   const int entry = unit / SUBS, b = entry / SPANS;
-  int f, lo, hi;
-  written(b, first, count, f, lo, hi);
+#define NEW(seq) (HAS_COUNT ? count[seq] : TOKENS)
+  // (of the entry that this thread looks through as well: two rounds of loads in all, the numbers and then pages and rows)
+  const int other = entry + 1 + tid, ob = min(other, SEQUENCES * SPANS - 1) / SPANS, f = first[b], n = NEW(b), of = first[ob], on = NEW(ob);
+  int lo, hi;
+  written(f, n, lo, hi);
   if (lo >= hi) return;
   const int lp = lo / SLOTS + entry % SPANS;
   if (lp >= TABLE) return;
   const int p0 = max(lo, lp * SLOTS + unit % SUBS * CHUNK), p1 = min(hi, min(lp * SLOTS + (unit % SUBS + 1) * CHUNK, (lp + 1) * SLOTS));
   if (p0 >= p1) return;
   const int page = table[(long long)b * TABLE + lp];
-  if ((u32)page >= (u32)PAGES) return;
-  if (tid == 0) clash = 0;
-  // the rows are on their way while the other pages are looked through
   const int lane = tid % LANES, rows = (p1 - p0) * HEADS_EACH;
   in_t kx[PASSES], vx[PASSES];
 #pragma unroll
@@ -132,27 +128,26 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
     kx[i] = take<DK>(k, src, lane);
     vx[i] = take<DV>(v, src, lane);
   }
+  int l, h, q;
+  bool same = written_page(min(other, SEQUENCES * SPANS - 1), of, on, table, l, h, q) == page && other < SEQUENCES * SPANS;
+  if ((u32)page >= (u32)PAGES) return;
+  if (tid == 0) clash = 0;
   __syncthreads();
-  bool same = false;
-  for (int e = entry + 1 + tid; e < SEQUENCES * SPANS; e += 256) {
-    int l, h, p;
-    same |= written_page(e, table, first, count, l, h, p) == page;
-  }
+  for (int e = other + 256; e < SEQUENCES * SPANS; e += 256) same |= written_page(e, first[e / SPANS], NEW(e / SPANS), table, l, h, q) == page;
   if (same) clash = 1;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
-    const int r = tid / LANES + i * (256 / LANES), p = p0 + r / HEADS_EACH, h = head0 + r % HEADS_EACH;
-    if (r >= rows || h >= HEADS) continue;
+    const int r = tid / LANES + i * (256 / LANES), p = p0 + r / HEADS_EACH, head = head0 + r % HEADS_EACH;
+    if (r >= rows || head >= HEADS) continue;
     if (clash) {
       bool later = false;
       for (int e = entry + 1; e < SEQUENCES * SPANS && !later; ++e) {
-        int l, hh, q0;
-        if (written_page(e, table, first, count, l, hh, q0) == page) later = q0 + p % SLOTS >= l && q0 + p % SLOTS < hh;
+        if (written_page(e, first[e / SPANS], NEW(e / SPANS), table, l, h, q) == page) later = q + p % SLOTS >= l && q + p % SLOTS < h;
       }
       if (later) continue;
     }
-    const long long dst = ((long long)page * HEADS + h) * SLOTS + p % SLOTS;
+    const long long dst = ((long long)page * HEADS + head) * SLOTS + p % SLOTS;
     put<DK>(k_pool, k_scale, kx[i], dst, lane);
     put<DV>(v_pool, v_scale, vx[i], dst, lane);
   }

@@ -43,6 +43,12 @@ def test_write_shapes(dtype, cache, DK, DV, HK, S):
     check_written(dg.write_graph(dtype, cache, 2 * S + 3, [1, 0, S - 1], [2 * S + 3, 2 * S, 1], HK=HK, DK=DK, DV=DV, S=S, M=4))
 
 
+@pytest.mark.parametrize("S", [1, 8, 100])
+def test_write_at_the_ends_of_the_number_range(S):
+    # positions around the largest and the smallest 32-bit number, behind the table, counts below zero and above the operand's tokens
+    check_written(dg.write_graph("bf16", "i8", 5, [2147483647, 2147483643, -2147483648, 6 * S - 2, -3, 0], [5, 2147483647, -1, 5, 2147483647, -2147483648], S=S))
+
+
 def test_write_leaves_out_pages_that_are_not_there():
     table = np.array([[0, -1, 3, 99, 2, 1], [4, 5, 6, 7, -2147483648, 2147483647]])
     check_written(dg.write_graph("bf16", "bf16", 40, [3, 1], table=table, P=8))

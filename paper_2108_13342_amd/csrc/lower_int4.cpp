@@ -32,7 +32,7 @@ typedef part_t frag_t __attribute__((ext_vector_type(8)));
 #define CHUNKS ((GK + CHUNK - 1) / CHUNK)
 #define ROW_BYTES ((GK + 1) / 2)
 #define PARTS_OF_CHUNK (4 / STEPS)                 // groups, or pieces of one, in a chunk
-#define ROWS (GM < 16 * MT ? GM : 16 * MT)
+#define ROWS (GM < 16 ? GM : 16)
 
 struct run_t {
   u32x4 w[NT];
@@ -89,7 +89,10 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   __shared__ __attribute__((aligned(16))) part_t xs[XP][ROWS][CHUNKS * CHUNK + 8];
 #endif
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
-  const idx_t c0 = (idx_t)blockIdx.x * (16 * NT), r0 = (idx_t)blockIdx.y * (16 * MT);
+  // The tiles of one column range, which read the same weights, lie eight workgroups apart: on one die, one after another.
+  const int group = blockIdx.x / (8 * ROW_TILES), member = blockIdx.x % (8 * ROW_TILES);
+  const idx_t c0 = (idx_t)(group * 8 + member % 8) * (16 * NT), r0 = (idx_t)(member / 8) * 16;
+  if (c0 >= GN) return;
   const unsigned char* __restrict__ wr[NT];
   const elem_t* __restrict__ sr[NT];
   const unsigned char* __restrict__ zr[NT];
@@ -103,9 +106,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #endif
   }
 #if !STAGED
-  const elem_t* __restrict__ xr[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) xr[t] = PX + offX_batch(0) + offX_row(min(r0 + t * 16 + n, (idx_t)(GM - 1)));
+  const elem_t* __restrict__ xr = PX + offX_batch(0) + offX_row(min(r0 + n, (idx_t)(GM - 1)));
 #endif
 
   auto load = [&](run_t& r, const int c) {
@@ -133,11 +134,9 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
     }
   };
 
-  f32x4 acc[MT][NT];
+  f32x4 acc[NT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int u = 0; u < NT; ++u) acc[t][u] = 0.0f;
+  for (int u = 0; u < NT; ++u) acc[u] = 0.0f;
   frag_t ones;
 #pragma unroll
   for (int j = 0; j < 8; ++j) ones[j] = (part_t)1.0f;
@@ -154,43 +153,33 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #endif
 #pragma unroll
     for (int p = 0; p < PARTS_OF_CHUNK; ++p) {
-      f32x4 sum[MT][NT], sx[MT];
+      f32x4 sum[NT], sx = 0.0f;
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        sx[t] = 0.0f;
-#pragma unroll
-        for (int u = 0; u < NT; ++u) sum[t][u] = 0.0f;
-      }
+      for (int u = 0; u < NT; ++u) sum[u] = 0.0f;
 #pragma unroll
       for (int i = p * STEPS; i < (p + 1) * STEPS; ++i) {
         const int k = c * CHUNK + (STEPS == 4 ? h * 32 + i * 8 : i * 32 + h * 8);
-        frag_t w[NT];
-#pragma unroll
-        for (int u = 0; u < NT; ++u) w[u] = decode(r.w[u][i]);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          frag_t x[XP];
+        frag_t x[XP];
 #if STAGED
 #pragma unroll
-          for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(t * 16 + n, ROWS - 1)][k];
+        for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(n, ROWS - 1)][k];
 #else
-          load_x(xr[t], k, x);
+        load_x(xr, k, x);
 #endif
 #pragma unroll
-          for (int q = 0; q < XP; ++q) {
-            sx[t] = MFMA(x[q], ones, sx[t], 0, 0, 0);
+        for (int q = 0; q < XP; ++q) sx = MFMA(x[q], ones, sx, 0, 0, 0);
 #pragma unroll
-            for (int u = 0; u < NT; ++u) sum[t][u] = MFMA(x[q], w[u], sum[t][u], 0, 0, 0);
-          }
+        for (int u = 0; u < NT; ++u) {
+          const frag_t w = decode(r.w[u][i]);
+#pragma unroll
+          for (int q = 0; q < XP; ++q) sum[u] = MFMA(x[q], w, sum[u], 0, 0, 0);
         }
       }
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
         const float s = cvt_in(r.s[u][p]), z = HAS_ZERO ? 16.0f + (float)r.z[u][p] : 24.0f;
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int e = 0; e < (ROWS < 4 ? ROWS : 4); ++e) acc[t][u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[t][e], sum[t][u][e]), acc[t][u][e]);
+        for (int e = 0; e < (ROWS < 4 ? ROWS : 4); ++e) acc[u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[e], sum[u][e]), acc[u][e]);
       }
     }
   };
@@ -220,12 +209,10 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 
   // ---- the wavefronts' sums, joined; result (4 h + e, n) of a 16x16 tile is element e
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int u = 0; u < NT; ++u)
 #pragma unroll
-    for (int u = 0; u < NT; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (t * 16 + 4 * h + e < ROWS) part[wave][t * 16 + 4 * h + e][u * 16 + n] = acc[t][u][e];
+    for (int e = 0; e < 4; ++e)
+      if (4 * h + e < ROWS) part[wave][4 * h + e][u * 16 + n] = acc[u][e];
   __syncthreads();
   for (int i = tid; i < ROWS * 16 * NT; i += 64 * WAVES) {
     const int rl = i / (16 * NT), cl = i % (16 * NT);
@@ -306,17 +293,20 @@ Lowered lower_int4(LowerCtx& c) {
   for (int t : params) wide = wide || g.tensors[t].n() >= (int64_t)1 << 31;
   wide = wide || M * N >= (int64_t)1 << 31;
 
-  // ---- tile: all rows up to 64; as many columns as leave two workgroups per compute unit; K split among up to sixteen
-  // wavefronts.  A product of one row is over before a long loop could settle: what counts is that all of its weights are asked
-  // for at once (11008 x 4096, bfloat16, one row: 9.6 us with sixteen wavefronts, 11.7 with eight, 14.3 with four).
-  const int64_t MT = std::min<int64_t>(4, (M + 15) / 16), row_tiles = (M + 16 * MT - 1) / (16 * MT), chunks = (K + 127) / 128;
+  // ---- tile: sixteen rows; K split among up to sixteen wavefronts.  A product of one row is over before a long loop could settle:
+  // what counts is that all of its weights are asked for at once (11008 x 4096, bfloat16, one row: 9.6 us with sixteen
+  // wavefronts, 11.7 with eight, 14.3 with four).
+  // Up to four rows x goes through LDS (one row, 4096 x 11008: 10.0 us, 14.3 with x read by every wavefront for itself; sixteen rows,
+  // 50257 x 768: 12.3 and 9.5) and a workgroup takes as many columns as leave two of them per compute unit.  With more rows
+  // it is x that the wavefronts wait for, and wide tiles read it less often: as many columns as leave 160 workgroups (16 rows,
+  // 11008 x 4096: 13.6 us with 64 columns, 18.5 with 16; 64 rows, 4096 x 4096: 11.8 and 22.3; but 16 rows, 4096 x 4096, where that
+  // would be 64 workgroups: 11.0 and 7.0).  Two or four row tiles a wavefront, for one pass over the codes, were no faster (64 rows,
+  // 4096 x 4096: 20.9 and 22.6 us).
+  const int64_t row_tiles = (M + 15) / 16, chunks = (K + 127) / 128, xp = X.dtype == DNNF_F32 ? 3 : 1;
+  const bool staged = xp * M <= 4 && xp * M * (chunks * 128 + 8) * 2 <= 40 * 1024;
   int64_t NT = 4;
-  while (NT > 1 && (N + 16 * NT - 1) / (16 * NT) * row_tiles < 512) NT /= 2;
+  while (NT > 1 && (N + 16 * NT - 1) / (16 * NT) * row_tiles < (staged ? 512 : 160)) NT /= 2;
   const int64_t most = std::min<int64_t>(16, chunks), each = (chunks + most - 1) / most, waves = (chunks + each - 1) / each, ahead = std::min<int64_t>(each, 2);
-  // x goes through LDS where that is less work than the weights that a workgroup reads (one row, 4096 x 11008: 10.0 us and 14.3 with
-  // x read by every wavefront for itself; sixteen rows, 50257 x 768: 12.3 and 9.5)
-  const int64_t xp = X.dtype == DNNF_F32 ? 3 : 1, staged_bytes = xp * std::min(M, 16 * MT) * (chunks * 128 + 8) * 2;
-  const bool staged = staged_bytes <= 40 * 1024 && staged_bytes * 10 <= 9 * (16 * NT * K / 2);
   const int steps = G % 128 == 0 || G >= K ? 4 : G % 64 == 0 ? 2 : 1;
 
   std::ostringstream k;
@@ -325,7 +315,7 @@ Lowered lower_int4(LowerCtx& c) {
   k << "#define ELEM_BYTES " << dtype_bytes(X.dtype) << "\n#define XP " << xp << "\n#define F16_PARTS " << (int)(X.dtype == DNNF_F16) << "\n";
   k << "#define MFMA __builtin_amdgcn_mfma_f32_16x16x32_" << (X.dtype == DNNF_F16 ? "f16" : "bf16") << "\n";
   k << "#define GM " << M << "\n#define GN " << N << "\n#define GK " << K << "\n#define GROUP " << G << "\n#define GROUPS " << groups << "\n#define HAS_ZERO " << (int)has_zero << "\n";
-  k << "#define MT " << MT << "\n#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define EACH " << each << "\n#define STAGED " << (int)staged << "\n#define STEPS " << steps << "\n";
+  k << "#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define ROW_TILES " << row_tiles << "\n#define EACH " << each << "\n#define STAGED " << (int)staged << "\n#define STEPS " << steps << "\n";
   k << "#define PX p0\n#define PW p1\n#define PS p2\n#define PZ p3\n";
   k << gemm_offset_fn(c, "offX_row", rows, xa) << gemm_offset_fn(c, "offX_batch", {}, xa);
   const std::string kparams = c.param_list(params, written);
@@ -340,9 +330,9 @@ Lowered lower_int4(LowerCtx& c) {
   L.ext_out.assign(params.begin() + n_in, params.end());
   Launch Kn;
   Kn.params = params;
-  Kn.grid[0] = (unsigned)((N + 16 * NT - 1) / (16 * NT));
-  DNNF_CHECK(row_tiles < 65536, DNNF_UNSUPPORTED_OP, "MatMulInt4: too many rows for one launch");
-  Kn.grid[1] = (unsigned)row_tiles;
+  const int64_t blocks = ((N + 16 * NT - 1) / (16 * NT) + 7) / 8 * 8 * row_tiles;
+  DNNF_CHECK(blocks < (int64_t)1 << 31, DNNF_UNSUPPORTED_OP, "MatMulInt4: more workgroups than one launch takes");
+  Kn.grid[0] = (unsigned)blocks;
   Kn.block[0] = (unsigned)(64 * waves);
   std::string src = std::string(device_preamble()) + k.str();
   Kn.name = fnv_name("dnnf_int4", src);
@@ -350,7 +340,7 @@ Lowered lower_int4(LowerCtx& c) {
   while ((pos = src.find("KNAME")) != std::string::npos) src.replace(pos, 5, Kn.name);
   Kn.source = src;
   L.launches.push_back(Kn);
-  L.variant = "int4_" + std::to_string(16 * MT) + "x" + std::to_string(16 * NT) + "_w" + std::to_string(waves) + "_g" + std::to_string(32 * steps);
+  L.variant = "int4_16x" + std::to_string(16 * NT) + "_w" + std::to_string(waves) + "_g" + std::to_string(32 * steps);
   return L;
 }
 

@@ -123,7 +123,8 @@ dnnf_status dnnf_graph_set_const(dnnf_graph* g, int tensor_id, const double* val
  *   MatMulInt4 (x, w, scale [, zero]) -> y     attribute "group_size" = G, a multiple of 32
  *       y [.., N] = sum over k of x [.., K] times (code[n, k] - zero[n, k / G]) * scale[n, k / G].  w is U8 [N, (K + 1) / 2], two codes a
  *       byte, the even k in the low half; scale [N, groups of K] is of x's type, zero U8 of that shape (8 where it is left
- *       out).  x has rank 2 or more and is finite (an infinity or NaN makes its row NaN).  One-to-One operators, Reshapes and
+ *       out).  x has rank 2 or more; 31 times the sum of a row's magnitudes is within
+ *       fp32 (a row for which it is not, one with an infinity or NaN among them, may come out as NaN).  One-to-One operators, Reshapes and
  *       Splits behind the product run in its kernel, as behind MatMul. */
 dnnf_status dnnf_graph_add_op(dnnf_graph* g, const char* op_kind, int n_in, const int* in_ids, int n_out,
                               const int* out_ids, const dnnf_attr* attrs, int n_attrs, int* op_id);

@@ -129,7 +129,7 @@ void check_decode_op(const Graph& g, const Op& op) {
   if (op.info->cls == OC_CACHE_ATTN) {
     const double w = op.f("window", 0), s = op.f("scale", 1);
     DNNF_CHECK(w >= 0 && w == (double)(int64_t)w && w < 2147483648.0, DNNF_INVALID_ARG, "CacheAttention: \"window\" is a number of keys, 0 for all");
-    DNNF_CHECK(s == s && s - s == 0, DNNF_INVALID_ARG, "CacheAttention: \"scale\" is no finite number");
+    DNNF_CHECK(s >= -1e38 && s <= 1e38, DNNF_INVALID_ARG, "CacheAttention: \"scale\" is no finite number");
   }
   if (op.info->cls != OC_CACHE_WRITE) return;
   // The pools are updated where they are: a result is its operand's buffer.  Nobody else may read the operand (which

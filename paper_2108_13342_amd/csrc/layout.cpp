@@ -31,7 +31,8 @@ int select_layouts(Graph& g) {
     const Tensor& T = g.tensors[t];
     if (T.kind != DNNF_INTERMEDIATE || T.weight_only || T.dims.size() != 4 || !is_float(T.dtype)) return false;
     if (T.dims[1] % vec_of(T)) return false;
-    auto flat = [&](int oi) { return g.ops[oi].info->cls == OC_RESHAPE; };
+    // (the cache operators and MatMulInt4 read and write rows as they are declared)
+    auto flat = [&](int oi) { return g.ops[oi].info->cls == OC_RESHAPE || is_decode_op(g.ops[oi]); };
     if (T.producer >= 0 && flat(T.producer)) return false;
     for (int oi : T.consumers) if (flat(oi)) return false;
     return true;

@@ -465,7 +465,7 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
     // a value's step goes to its probability, relative to the largest step of these keys (float16 has the range for nothing else)
     float unit = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) unit = fmaxf(unit, t.vs[j / 4][j % 4]);
+    for (int j = 0; j < 8; ++j) unit = fmaxf(unit, __builtin_fabsf(t.vs[j / 4][j % 4]));
     unit = fmaxf(unit, __shfl_xor(unit, 16, 64));
     unit = fmaxf(unit, __shfl_xor(unit, 32, 64));
     const float per_unit = unit > 0.0f ? dn_rcp(unit) : 0.0f;

@@ -405,6 +405,100 @@ def test_two_runs_are_alike_bit_for_bit():
                 np.testing.assert_array_equal(got[n], again[n])
 
 
+def test_a_cached_prefix_continued_by_ordinary_products():
+    """A chunk of new tokens written behind a cached prefix, everything read back, and attended over with MatMul - Softmax - MatMul
+    (as one streaming block and as separate kernels)."""
+    from parity import TOL, rel_err
+
+    for attention in (0, 1):
+        spec = dg.write_graph("f16", "i8", 16, [48, 48], HK=2, DK=64, DV=64, S=16, M=4)
+        b = dg.GraphBuilder("prefix", "f16")
+        b.g = spec
+        kept = list(spec.ops[0].outputs)
+        held = b.input("held", (2,), np.array([64, 64]), dtype="i32")
+        k, v = (b._add(n, "f16", (2, 64, 2, 64), "intermediate") for n in ("k_all", "v_all"))
+        b.g.ops.append(dg.OpSpec("CacheRead", kept + ["table", held], [k, v], {"length": 64}))
+        q = b.input("q", (2, 2, 16, 64), dg.normal(9, 1, (2, 2, 16, 64), "f16"))
+        kt = b.op("Transpose", [k], (2, 2, 64, 64), {"perm": [0, 2, 3, 1]})
+        vt = b.op("Transpose", [v], (2, 2, 64, 64), {"perm": [0, 2, 1, 3]})
+        s = b.op("Mul", [b.op("MatMul", [q, kt], (2, 2, 16, 64)), b.const("scale", 0.125)], (2, 2, 16, 64))
+        mask = np.where(np.arange(64)[None, :] <= 48 + np.arange(16)[:, None], 0.0, -10000.0)
+        s = b.op("Add", [s, b.input("mask", (16, 64), dg.rng.round_to(mask, "f16"))], (2, 2, 16, 64))
+        b.mark_output(b.op("MatMul", [b.op("Softmax", [s], (2, 2, 16, 64), {"axis": -1}), vt], (2, 2, 16, 64), out_names=["o"]))
+        spec.tensors["o"].kind = "output"
+        session, got = run(spec, attention=attention)
+        assert any(d["family"] == 6 for d in session.plan.describe()) == bool(attention)
+        assert rel_err(got["o"], run_graph(spec)["o"]) <= TOL["f16"]
+
+
+@pytest.mark.parametrize("how", ["slice", "transpose", "split", "reshape"])
+def test_int4_of_a_view(how):
+    """x as a part, another order or another shape of what is stored: folded into the addresses, or stored first."""
+    b = dg.GraphBuilder("view", "bf16")
+    K, N = 96, 40
+    if how == "slice":
+        x = b.op("Slice", [b.input("in", (7, 2 * K + 3), dg.normal(5, 1, (7, 2 * K + 3), "bf16"))], (5, K), {"starts": [1, 3], "ends": [6, 3 + K], "axes": [0, 1]})
+    elif how == "transpose":
+        x = b.op("Transpose", [b.input("in", (K, 5), dg.normal(5, 1, (K, 5), "bf16"))], (5, K), {"perm": [1, 0]})
+    elif how == "split":
+        x = b.op("Split", [b.input("in", (5, 3 * K), dg.normal(5, 1, (5, 3 * K), "bf16"))], [(5, K)] * 3, {"axis": 1, "split": [K] * 3})[1]
+    else:
+        x = b.op("Reshape", [b.input("in", (5, 4, K // 4), dg.normal(5, 1, (5, 4, K // 4), "bf16"))], (5, K), {"shape": [5, K]})
+    w = b.weight("w", (N, K // 2), dg.rng.integers(5, 2, (N, K // 2), 0, 256), dtype="u8")
+    s = b.weight("s", (N, K // 32), dg.rng.round_to(dg.rng.uniform(5, 3, (N, K // 32), 0.01, 0.05), "bf16"))
+    b.mark_output(b.op("MatMulInt4", [x, w, s], (5, N), {"group_size": 32}))
+    spec = b.finish()
+    env = run_graph(spec, keep="all")
+    terms = np.abs(env[x]) @ np.repeat(data(spec, "s"), 32, axis=1).T
+    for kw in ({}, {"fusion": 0}, {"intra_block": 0}):
+        _, got = run(spec, **kw)
+        for n, y in got.items():
+            assert np.all(np.abs(y - env[n]) <= 2.0 ** -8 * np.abs(env[n]) * 1.01 + 2.0 ** -24 * (K + 16) * 62 * terms), (how, kw)
+
+
+def test_replayed_by_the_plan_itself():
+    """The plan option `graphs`: the run loop with an in-place cache becomes a graph on the second run and follows its buffers."""
+    import torch
+
+    from paper_2108_13342_amd import api
+    from workloads import configs
+
+    spec = configs.gpt2_decode_step(**configs.SMALL_EXTRA["gpt2_decode_step"], cache="i8")
+    one, two = api.Session(spec, graphs=0), api.Session(spec, graphs=1)
+    ids = [i for i, t in enumerate(t for t in spec.tensors.values() if t.kind == "input") if t.name in ("input_ids", "position", "held")]
+    for step in range(5):
+        for s in (one, two):
+            s.run()
+        torch.cuda.synchronize()
+        for x, y in zip(one.outputs[0], two.outputs[0]):
+            assert torch.equal(x, y), f"step {step}"
+        for s in (one, two):
+            s.inputs[0][ids[0]].add_(7).remainder_(211)
+            for i in ids[1:]:
+                s.inputs[0][i].add_(1)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "i8"])
+def test_nothing_held_at_all(cache):
+    for M in (1, 60):
+        _, got = run(dg.attend_graph("bf16", cache, [0, 0, -1], S=16, M=M))
+        assert np.all(got["o"] == 0.0)
+
+
+def test_steps_of_either_sign():
+    """A cache of 8 bits that somebody else filled, with negative steps."""
+    spec = dg.attend_graph("f16", "i8", [100, 31], S=16, M=8)
+    for n in ("k_scale", "v_scale"):
+        t = spec.tensors[n]
+        t.data = np.where(np.arange(t.data.size).reshape(t.data.shape) % 3 == 0, -t.data, t.data)
+    _, got = run(spec)
+    want = run_graph(spec)["o"]
+    # |o - o64|: the result's rounding, and fp32 sums (98 roundings a step of sums up to 255 steps, scores to (64 + 8) 2^-24 sum |q k|)
+    q, ks, vs = data(spec, "q"), data(spec, "k_scale"), data(spec, "v_scale")
+    score = np.abs(q).sum(-1).max() * 127 * np.abs(ks).max() / 8
+    assert np.all(np.abs(got["o"] - want) <= 2.0 ** -11 * np.abs(want) * 1.01 + 2.0 ** -24 * (98 * 255 + 127 * (2 * 72 * score + 16 + 128)) * np.abs(vs).max())
+
+
 def test_in_place_results_take_their_operand_s_buffer():
     from paper_2108_13342_amd import api
 

@@ -119,6 +119,21 @@ def test_casts_next_to_typed_operands_stay():
     api.Plan(g, [1] * 2)
 
 
+def test_data_format_selection_leaves_cache_rows_alone():
+    """A convolution's result that goes into the cache keeps the declared order; the one in front of it need not."""
+    b = dg.GraphBuilder("conv_cache", "f16")
+    x = b.input("x", (2, 16, 8, 32), dg.normal(1, 1, (2, 16, 8, 32), "f16"))
+    w = [b.weight(f"w{i}", (16, 16, 3, 3), dg.normal(2, i, (16, 16, 3, 3), "f16")) for i in range(2)]
+    conv = {"strides": [1, 1], "pads": [1, 1, 1, 1], "group": 1}
+    y = b.op("Relu", [b.op("Conv", [b.op("Relu", [b.op("Conv", [x, w[0]], (2, 16, 8, 32), conv)], (2, 16, 8, 32)), w[1]], (2, 16, 8, 32), conv)], (2, 16, 8, 32))
+    table, P = dg.pages_of(5, 2, 2)
+    pools = dg.pool_inputs(b, 5, "f16", P, 8, 16, 32, 32)
+    ins = pools + [y, y, b.input("table", table.shape, table, dtype="i32"), b.input("first", (2,), np.array([0, 3]), dtype="i32")]
+    b.g.ops.append(dg.OpSpec("CacheWrite", ins, [b._add(p + "_new", "f16", b.shape(p), "output") for p in pools]))
+    p = plan(b.finish(), layout=1)
+    assert [d["ops"] for d in p.describe() if not d["prepare_only"]][-1] == ["CacheWrite"]
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 def refused(spec, match, code=None):
     with pytest.raises(api.DnnfError, match=match) as e:
@@ -160,6 +175,7 @@ INVALID, MISMATCH, UNSUPPORTED = -1, -2, -3
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": -1}), "window", INVALID),
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": 2.5}), "window", INVALID),
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"scale": float("nan")}), "scale", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"scale": 1e39}), "scale", INVALID),
     (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=0), "length", INVALID),
     (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=5), "declared", MISMATCH),
     (lambda: retyped(dg.read_graph("f16", "f16", [1], 4), "k_out", "f32"), "share one type", INVALID),

@@ -25,7 +25,8 @@ namespace {
 const char* kInt4Body = R"KRN(
 typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
-typedef u32x4 u32x4_any __attribute__((aligned(1)));
+typedef u32x4 u32x4_any __attribute__((aligned(4)));
+typedef u32x4 u32x4_byte __attribute__((aligned(1)));
 typedef elem_t xvec_t __attribute__((ext_vector_type(8), aligned(ELEM_BYTES)));
 typedef part_t frag_t __attribute__((ext_vector_type(8)));
 #define CHUNK 128                                  // codes of a row that a wavefront reads at once
@@ -40,18 +41,56 @@ struct run_t {
   unsigned char z[NT][PARTS_OF_CHUNK];
 };
 
+// 16 bytes from any address: the five words around them, moved together (vector loads off a word's boundary are taken apart by the
+// hardware).  Reads up to 4 bytes behind them.
+DEV u32x4 load_16(const void* p) {
+  const unsigned long long at = (unsigned long long)p;
+  const u32* __restrict__ q = (const u32*)(at & ~3ull);
+  const u32x4 w = *(const u32x4_any*)q;
+  const u32 last = q[4], off = (u32)at & 3u;
+  return (u32x4){__builtin_amdgcn_alignbyte(w[1], w[0], off), __builtin_amdgcn_alignbyte(w[2], w[1], off), __builtin_amdgcn_alignbyte(w[3], w[2], off),
+                 __builtin_amdgcn_alignbyte(last, w[3], off)};
+}
+// 16 bytes moved down by some of them; zeros follow
+DEV u32x4 move_down(const u32x4 v, const int bytes) {
+  typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+  const u64x2 w = __builtin_bit_cast(u64x2, v);
+  const int s = bytes * 8;
+  u64x2 r;
+  r[0] = s == 0 ? w[0] : s < 64 ? w[0] >> s | w[1] << (64 - s) : s < 128 ? w[1] >> (s & 63) : 0;
+  r[1] = s < 64 ? w[1] >> (s & 63) : 0;
+  return __builtin_bit_cast(u32x4, r);
+}
+
+// Whether all of a chunk of x lies inside K: then no vector of it needs a look.  (A branch of the whole wavefront, once a chunk.)
+struct whole_t { static constexpr bool whole = true; };
+struct cut_t { static constexpr bool whole = false; };
+
 // x[row, k .. k + 8) in the order of a word's codes, in XP parts
-DEV void load_x(const elem_t* __restrict__ xr, const int k, frag_t (&f)[XP]) {
+template <typename T> DEV void load_x(const elem_t* __restrict__ xr, const int k, frag_t (&f)[XP], T) {
   float v[8];
   elem_t e[8];
-  if (GK % 8 == 0 ? (GK % CHUNK == 0 || k < GK) : k + 8 <= GK) {
-    const xvec_t t = *(const xvec_t*)(xr + k);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = t[j];
+#if XP == 1
+  u32x4 t;
+  if (T::whole) t = X_WORDS ? *(const u32x4_any*)(xr + k) : load_16(xr + k);
+  else if (GK >= 8) {                                            // the last eight of the row, moved to where they belong
+    const int at = min(k, GK - 8);
+    t = move_down(__builtin_bit_cast(u32x4, *(const xvec_t*)(xr + at)), min(k - at, 8) * 2);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { e[j] = 0; if (k + j < GK) e[j] = xr[k + j]; }
+    for (int j = 0; j < 8; ++j) { const elem_t y = xr[min(k + j, GK - 1)]; e[j] = k + j < GK ? y : (elem_t)0; }
+    t = __builtin_bit_cast(u32x4, (xvec_t){e[0], e[1], e[2], e[3], e[4], e[5], e[6], e[7]});
   }
+  const xvec_t all = __builtin_bit_cast(xvec_t, t);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = all[j];
+#else
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (T::whole) e[j] = xr[k + j];
+    else { const elem_t y = xr[min(k + j, GK - 1)]; e[j] = k + j < GK ? y : (elem_t)0; }
+  }
+#endif
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int slot = j < 4 ? 2 * j : 2 * (j - 4) + 1;
@@ -110,18 +149,23 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #endif
 
   auto load = [&](run_t& r, const int c) {
+    // (load_16, for rows that begin off a word's boundary, reads a word too much)
+    const int more = ROW_BYTES % 4 == 0 ? 0 : 4;
+    const bool whole = ROW_BYTES % 64 == 0 || (c + 1) * (CHUNK / 2) + more <= ROW_BYTES;
     const int at = c * (CHUNK / 2) + h * 16;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if (ROW_BYTES % 64 == 0 || at + 16 <= ROW_BYTES) r.w[t] = *(const u32x4_any*)(wr[t] + at);
-      else {
-        // the end of a row (codes behind it are multiplied by zeros)
+      if (whole) r.w[t] = ROW_BYTES % 4 == 0 ? *(const u32x4_any*)(wr[t] + at) : load_16(wr[t] + at);
+      else if ((long long)GN * ROW_BYTES >= 16) {
+        // The end of a row, and what lies behind it: the next row's codes, which meet zeros of x.  Behind the last row there is
+        // nothing: the last bytes of all, moved to where they belong.
+        const long long want = wr[t] - PW + at, from = min(want, (long long)GN * ROW_BYTES - 16);
+        r.w[t] = move_down(*(const u32x4_byte*)(PW + from), (int)min(want - from, 16ll));
+      } else {
         r.w[t] = 0;
-        if (ROW_BYTES % 16 != 0) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (at + i < ROW_BYTES) r.w[t][i / 4] |= (u32)wr[t][at + i] << (i % 4 * 8);
-        }
+        for (int i = 0; i < 16; ++i)
+          if (at + i < ROW_BYTES) r.w[t][i / 4] |= (u32)wr[t][at + i] << (i % 4 * 8);
       }
 #pragma unroll
       for (int p = 0; p < PARTS_OF_CHUNK; ++p) {
@@ -141,7 +185,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) ones[j] = (part_t)1.0f;
 
-  auto multiply = [&](run_t& r, const int c) {
+  auto multiply = [&](run_t& r, const int c, auto reach) {
 #if STEPS < 4
     // words (quarter q, register i) -> (quarter i, register q)
 #pragma unroll
@@ -164,7 +208,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
 #pragma unroll
         for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(n, ROWS - 1)][k];
 #else
-        load_x(xr, k, x);
+        load_x(xr, k, x, reach);
 #endif
 #pragma unroll
         for (int q = 0; q < XP; ++q) sx = MFMA(x[q], ones, sx, 0, 0, 0);
@@ -193,7 +237,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   for (int i = tid; i < ROWS * (CHUNKS * 16); i += 64 * WAVES) {
     const int r = i / (CHUNKS * 16), k = i % (CHUNKS * 16) * 8;
     frag_t x[XP];
-    load_x(PX + offX_batch(0) + offX_row(min(r0 + r, (idx_t)(GM - 1))), k, x);
+    load_x(PX + offX_batch(0) + offX_row(min(r0 + r, (idx_t)(GM - 1))), k, x, cut_t());
 #pragma unroll
     for (int q = 0; q < XP; ++q) *(frag_t*)&xs[q][r][k] = x[q];
   }
@@ -202,7 +246,10 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   for (int c = first; c < last; c += AHEAD) {
 #pragma unroll
     for (int p = 0; p < AHEAD; ++p) {
-      if (c + p < last) multiply(ring[p], c + p);
+      if (c + p < last) {
+        if ((X_WORDS && GK % CHUNK == 0) || (c + p + 1) * CHUNK + (X_WORDS ? 0 : 2) <= GK) multiply(ring[p], c + p, whole_t());
+        else multiply(ring[p], c + p, cut_t());
+      }
       if (EACH > AHEAD) load(ring[p], min(c + p + AHEAD, last - 1));      // (unconditional: loads behind a branch make the next wait one for all)
     }
   }
@@ -316,6 +363,10 @@ Lowered lower_int4(LowerCtx& c) {
   k << "#define MFMA __builtin_amdgcn_mfma_f32_16x16x32_" << (X.dtype == DNNF_F16 ? "f16" : "bf16") << "\n";
   k << "#define GM " << M << "\n#define GN " << N << "\n#define GK " << K << "\n#define GROUP " << G << "\n#define GROUPS " << groups << "\n#define HAS_ZERO " << (int)has_zero << "\n";
   k << "#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define ROW_TILES " << row_tiles << "\n#define EACH " << each << "\n#define STAGED " << (int)staged << "\n#define STEPS " << steps << "\n";
+  // x's rows, and what they are a part of, begin on words' boundaries
+  bool x_words = xa.offset % 2 == 0;
+  for (int a : rows) x_words = x_words && stride_of(xa, a) % 2 == 0;
+  k << "#define X_WORDS " << (int)(x_words || X.dtype == DNNF_F32) << "\n";
   k << "#define PX p0\n#define PW p1\n#define PS p2\n#define PZ p3\n";
   k << gemm_offset_fn(c, "offX_row", rows, xa) << gemm_offset_fn(c, "offX_batch", {}, xa);
   const std::string kparams = c.param_list(params, written);

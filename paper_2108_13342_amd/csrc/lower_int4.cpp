@@ -12,6 +12,8 @@
 //     four steps as they are (each step meets all four quarters of the run).  Smaller groups have to meet 32 successive codes in a step:
 //     four exchanges between the wavefront's quarters turn the 4 x 4 words around.
 //   - fp32 x is taken in three bfloat16 parts, which hold all of its 24 bits; weights are exact in either case.
+// One row of 4096 x 11008 (groups of 128, bfloat16): 23.6 MB in 8.7 us, 2.7 TB/s; 50257 x 768 for 16 rows 21.5 MB in 8.9 us.  A kernel that
+// only has to be launched takes 2 us, its first loads another 2, and the bytes 4; nothing of this overlaps in so short a run.
 // The wavefronts of a workgroup share its columns and split K among them; sums are joined in LDS in a fixed order.
 #include <algorithm>
 #include <sstream>

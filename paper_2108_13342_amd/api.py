@@ -258,11 +258,13 @@ class BoundPlan:
 
     def __init__(self, plan: Plan, inputs, outputs, workspace: int):
         self._plan = plan
-        self._args = (plan._h, plan._ptrs(inputs), plan._ptrs(outputs), C.c_void_p(workspace or None))
+        self._h, self._in, self._out, self._ws = plan._h, plan._ptrs(inputs), plan._ptrs(outputs), C.c_void_p(workspace or None)
         self._run = _lib.lib().dnnf_plan_run
 
     def run(self, stream: int = 0):
-        _check(self._run(*self._args, stream or None))
+        rc = self._run(self._h, self._in, self._out, self._ws, stream or None)
+        if rc:
+            _check(rc)
 
 
 def precompile_spec(spec, fusion=1, rewrite=True, cache_dir=None, tune=0, attention=0, layout=0, broadcast_prologue=0, gemm_norm=0, squeeze_excite=0) -> int:

@@ -9,6 +9,12 @@ bool is_decode_op(const Op& op) {
   return c == OC_CACHE_WRITE || c == OC_CACHE_READ || c == OC_CACHE_ATTN || c == OC_MATMUL_INT4;
 }
 
+// An attribute that counts something; -1 where it is no whole number below 2^31.
+static int64_t whole_attr(const Op& op, const char* name) {
+  const double v = op.f(name, 0);
+  return v >= 0 && v < 2147483648.0 && v == (double)(int64_t)v ? (int64_t)v : -1;
+}
+
 // Operand order
 //   CacheWrite      k_pool, v_pool, [k_scale, v_scale,] k, v, table, first [, count]  ->  k_pool, v_pool [, k_scale, v_scale]
 //   CacheRead       k_pool, v_pool, [k_scale, v_scale,] table, held                   ->  k, v
@@ -57,7 +63,7 @@ CacheOperands cache_operands(const Graph& g, const Op& op) {
     for (int i = 0; i < 2; i++) agree(dims(c.fresh[i]) == Dims{c.B, c.T, c.HK, c.D[i]}, "new keys / values differ from the pools or the table");
   }
   if (cls == OC_CACHE_READ) {
-    c.T = op.i("length", 0);
+    c.T = whole_attr(op, "length");
     DNNF_CHECK(c.T >= 1, DNNF_INVALID_ARG, "CacheRead needs \"length\", the positions laid out");
   }
   if (cls == OC_CACHE_ATTN) {
@@ -75,7 +81,7 @@ Dims infer_decode_shape(const Graph& g, const Op& op, int oi) {
     DNNF_CHECK(op.out.size() == 1, DNNF_INVALID_ARG, "MatMulInt4 has one result");
     const Dims &x = g.tensors[op.in[0]].dims, &w = g.tensors[op.in[1]].dims;
     DNNF_CHECK(x.size() >= 2 && w.size() == 2, DNNF_SHAPE_MISMATCH, "MatMulInt4: x is [.., rows, K], weights [N, K / 2]");
-    const int64_t K = x.back(), G = op.i("group_size", 0);
+    const int64_t K = x.back(), G = whole_attr(op, "group_size");
     DNNF_CHECK(G >= 32 && G % 32 == 0, DNNF_INVALID_ARG, "MatMulInt4 needs \"group_size\", a multiple of 32");
     DNNF_CHECK(w[1] == (K + 1) / 2, DNNF_SHAPE_MISMATCH, "MatMulInt4: a row of weights is (K + 1) / 2 bytes");
     for (size_t i = 2; i < op.in.size(); i++)
@@ -127,8 +133,8 @@ void check_decode_op(const Graph& g, const Op& op) {
   DNNF_CHECK(is_float(type(rows[0])) && type(rows[1]) == type(rows[0]) && (c.eight_bits || type(rows[0]) == pooled), DNNF_INVALID_ARG,
              op.kind + ": its float operands share one type, which is the pools' unless those are I8");
   if (op.info->cls == OC_CACHE_ATTN) {
-    const double w = op.f("window", 0), s = op.f("scale", 1);
-    DNNF_CHECK(w >= 0 && w == (double)(int64_t)w && w < 2147483648.0, DNNF_INVALID_ARG, "CacheAttention: \"window\" is a number of keys, 0 for all");
+    const double s = op.f("scale", 1);
+    DNNF_CHECK(whole_attr(op, "window") >= 0, DNNF_INVALID_ARG, "CacheAttention: \"window\" is a number of keys, 0 for all");
     DNNF_CHECK(s >= -1e38 && s <= 1e38, DNNF_INVALID_ARG, "CacheAttention: \"scale\" is no finite number");
   }
   if (op.info->cls != OC_CACHE_WRITE) return;

@@ -176,6 +176,11 @@ INVALID, MISMATCH, UNSUPPORTED = -1, -2, -3
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": 2.5}), "window", INVALID),
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"scale": float("nan")}), "scale", INVALID),
     (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"scale": 1e39}), "scale", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": 1e30}), "window", INVALID),
+    (lambda: dg.attend_graph("bf16", "bf16", [1], attrs={"window": float("nan")}), "window", INVALID),
+    (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=4.5), "length", INVALID),
+    (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=-1e300), "length", INVALID),
+    (lambda: with_attrs(dg.int4_graph("f16", (1,), 64, 8, 32), group_size=float("inf")), "group_size", INVALID),
     (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=0), "length", INVALID),
     (lambda: with_attrs(dg.read_graph("f16", "f16", [1], 4), length=5), "declared", MISMATCH),
     (lambda: retyped(dg.read_graph("f16", "f16", [1], 4), "k_out", "f32"), "share one type", INVALID),
@@ -245,3 +250,25 @@ def test_sizes_beyond_the_index_ranges():
         declared(1 << 24, 16, 4)
     with pytest.raises(api.DnnfError, match="2\\^30 positions"):
         declared(16, 1024, 1 << 20)
+
+
+def test_host_code_under_sanitizers(tmp_path):
+    """Checks, plans and generated sources of these operators, refusals among them, through the instrumented library."""
+    from test_host_sanitizers import run, write_spec
+
+    from paper_2108_13342_amd import build
+    from workloads import configs
+
+    fine = {"decode_step": configs.gpt2_decode_step(**configs.SMALL_EXTRA["gpt2_decode_step"]), "write": dg.write_graph("f32", "i8", 40, [0, 7]),
+            "read": dg.read_graph("bf16", "bf16", [3], 20), "attend": dg.attend_graph("f32", "i8", [9], HQ=34, M=80, DV=112),
+            "int4": dg.int4_graph("f32", (3, 2), 77, 40, 32, True, bias=True)}
+    bad = {"window": (dg.attend_graph("bf16", "bf16", [1], attrs={"window": 1e30}), -1), "heads": (reshaped(dg.attend_graph("bf16", "bf16", [1, 1]), "q", (2, 3, 64)), -2),
+           "channels": (dg.attend_graph("bf16", "bf16", [1], DK=40), -3), "group": (with_attrs(dg.int4_graph("f16", (1,), 64, 8, 32), group_size=1e30), -1)}
+    files = []
+    for name, (spec, code) in {**{n: (s, 0) for n, s in fine.items()}, **bad}.items():
+        files.append(str(tmp_path / (name + ".txt")))
+        write_spec(spec, files[-1], expect_finalize=code)
+    r = run(build.build_sanitizer_driver(), files)
+    assert r.returncode == 0, (r.stdout[-2000:], r.stderr[-6000:])
+    assert "Sanitizer" not in r.stderr and "runtime error" not in r.stderr, r.stderr[-6000:]
+    assert r.stdout.count("\nok ") + r.stdout.startswith("ok ") == len(files), r.stdout

@@ -8,9 +8,15 @@
 //     that the results have, so that a group costs two fp32 instructions per result.  (Infinite or NaN x: the row is NaN.)
 //   - The order of k within a contraction step is free as long as both operands have the same: a lane takes the codes in the order
 //     in which they leave a 32-bit word (0, 4, 1, 5, 2, 6, 3, 7), and x is picked in that order.
-//   - A wavefront reads 16 weight rows, 16 bytes a lane: 128 codes a row.  In groups of 128 and more a lane's 32 codes go into
-//     four steps as they are (each step meets all four quarters of the run).  Smaller groups have to meet 32 successive codes in a step:
-//     four exchanges between the wavefront's quarters turn the 4 x 4 words around.
+//   - A wavefront reads 16 weight rows, 16 bytes a lane: 128 codes a row.  In groups of 128 and more, x in LDS, a lane's 32
+//     codes go into four steps as they are (each step meets all four quarters of the run).  Smaller groups have to meet 32 successive
+//     codes in a step: four exchanges between the wavefront's quarters turn the 4 x 4 words around.  So they do where x comes from
+//     memory: a load then touches 64 bytes of each of its rows and not 16 of every 64 (16 rows, 11008 x 4096: 17.2 us, 20.7 unturned).
+//   - Scales and zeros lie a row of groups apart: a load of theirs touches sixteen lines, and such loads, not bytes, are what a
+//     compute unit runs out of.  Where groups fill a chunk evenly, one vector holds all that the chunk needs.  Elsewhere (groups of
+//     96, an odd count) each quarter of the wavefront loads the group of its own quarter of the chunk, and exchanges give it to all: 16 rows,
+//     4096 x 11008 in groups of 96: 13.8 us, 39.5 with a load for every part.  (In groups of 32, 4096 x 4096, the vector takes 7.8 us, the
+//     exchanges 8.6.)
 //   - fp32 x is taken in three bfloat16 parts, which hold all of its 24 bits; weights are exact in either case.
 // One row of 4096 x 11008 (groups of 128, bfloat16): 23.6 MB in 8.7 us, 2.7 TB/s; 50257 x 768 for 16 rows 21.5 MB in 8.9 us.  A kernel that
 // only has to be launched takes 2 us, its first loads another 2, and the bytes 4; nothing of this overlaps in so short a run.
@@ -37,10 +43,15 @@ typedef part_t frag_t __attribute__((ext_vector_type(8)));
 #define PARTS_OF_CHUNK (4 / STEPS)                 // groups, or pieces of one, in a chunk
 #define ROWS (GM < 16 ? GM : 16)
 
+// what a lane reads of a chunk's scales and zeros: those of all its parts or, to SPREAD, those of quarter h's group
+#define READ (SPREAD ? 1 : PARTS_OF_CHUNK)
+typedef elem_t scales_t __attribute__((ext_vector_type(READ), aligned(ELEM_BYTES)));
+typedef unsigned char zeros_t __attribute__((ext_vector_type(READ), aligned(1)));
+
 struct run_t {
   u32x4 w[NT];
-  elem_t s[NT][PARTS_OF_CHUNK];
-  unsigned char z[NT][PARTS_OF_CHUNK];
+  scales_t s[NT];
+  zeros_t z[NT];
 };
 
 // 16 bytes from any address: the five words around them, moved together (vector loads off a word's boundary are taken apart by the
@@ -67,6 +78,23 @@ DEV u32x4 move_down(const u32x4 v, const int bytes) {
 // Whether all of a chunk of x lies inside K: then no vector of it needs a look.  (A branch of the whole wavefront, once a chunk.)
 struct whole_t { static constexpr bool whole = true; };
 struct cut_t { static constexpr bool whole = false; };
+
+#if SPREAD
+// the values that the quarters of a chunk's parts hold, for all lanes
+DEV void spread(const u32 v, u32 (&r)[PARTS_OF_CHUNK]) {
+  const u32x2 a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+#if STEPS == 2
+  r[0] = a[0];
+  r[1] = a[1];
+#else
+  const u32x2 p = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false), q = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
+  r[0] = p[0];
+  r[1] = p[1];
+  r[2] = q[0];
+  r[3] = q[1];
+#endif
+}
+#endif
 
 // x[row, k .. k + 8) in the order of a word's codes, in XP parts
 template <typename T> DEV void load_x(const elem_t* __restrict__ xr, const int k, frag_t (&f)[XP], T) {
@@ -169,14 +197,15 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
         for (int i = 0; i < 16; ++i)
           if (at + i < ROW_BYTES) r.w[t][i / 4] |= (u32)wr[t][at + i] << (i % 4 * 8);
       }
-#pragma unroll
-      for (int p = 0; p < PARTS_OF_CHUNK; ++p) {
-        const int g = min((c * CHUNK + p * STEPS * 32) / GROUP, GROUPS - 1);
-        r.s[t][p] = sr[t][g];
-#if HAS_ZERO
-        r.z[t][p] = zr[t][g];
+#if SPREAD || STEPS == 4
+      const int g = (c * CHUNK + (SPREAD ? h * 32 : 0)) / GROUP, at_g = SPREAD ? min(g, GROUPS - 1) : g;
+#else
+      const int at_g = c * PARTS_OF_CHUNK;
 #endif
-      }
+      r.s[t] = *(const scales_t*)(sr[t] + at_g);
+#if HAS_ZERO
+      r.z[t] = *(const zeros_t*)(zr[t] + at_g);
+#endif
     }
   };
 
@@ -188,13 +217,23 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   for (int j = 0; j < 8; ++j) ones[j] = (part_t)1.0f;
 
   auto multiply = [&](run_t& r, const int c, auto reach) {
-#if STEPS < 4
+#if TURNED
     // words (quarter q, register i) -> (quarter i, register q)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const u32x2 a = __builtin_amdgcn_permlane32_swap(r.w[t][0], r.w[t][2], false, false), b = __builtin_amdgcn_permlane32_swap(r.w[t][1], r.w[t][3], false, false);
       const u32x2 p = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), q = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
       r.w[t] = (u32x4){p[0], p[1], q[0], q[1]};
+    }
+#endif
+#if SPREAD
+    u32 scale[NT][PARTS_OF_CHUNK], zero[NT][PARTS_OF_CHUNK];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      spread(__builtin_bit_cast(u32, cvt_in(r.s[u][0])), scale[u]);
+#if HAS_ZERO
+      spread(__builtin_bit_cast(u32, 16.0f + (float)r.z[u][0]), zero[u]);
+#endif
     }
 #endif
 #pragma unroll
@@ -204,7 +243,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
       for (int u = 0; u < NT; ++u) sum[u] = 0.0f;
 #pragma unroll
       for (int i = p * STEPS; i < (p + 1) * STEPS; ++i) {
-        const int k = c * CHUNK + (STEPS == 4 ? h * 32 + i * 8 : i * 32 + h * 8);
+        const int k = c * CHUNK + (TURNED ? i * 32 + h * 8 : h * 32 + i * 8);
         frag_t x[XP];
 #if STAGED
 #pragma unroll
@@ -223,7 +262,11 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
       }
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
+#if SPREAD
+        const float s = __builtin_bit_cast(float, scale[u][p]), z = HAS_ZERO ? __builtin_bit_cast(float, zero[u][p]) : 24.0f;
+#else
         const float s = cvt_in(r.s[u][p]), z = HAS_ZERO ? 16.0f + (float)r.z[u][p] : 24.0f;
+#endif
 #pragma unroll
         for (int e = 0; e < (ROWS < 4 ? ROWS : 4); ++e) acc[u][e] = __builtin_fmaf(s, __builtin_fmaf(-z, sx[e], sum[u][e]), acc[u][e]);
       }
@@ -365,10 +408,13 @@ Lowered lower_int4(LowerCtx& c) {
   k << "#define MFMA __builtin_amdgcn_mfma_f32_16x16x32_" << (X.dtype == DNNF_F16 ? "f16" : "bf16") << "\n";
   k << "#define GM " << M << "\n#define GN " << N << "\n#define GK " << K << "\n#define GROUP " << G << "\n#define GROUPS " << groups << "\n#define HAS_ZERO " << (int)has_zero << "\n";
   k << "#define NT " << NT << "\n#define WAVES " << waves << "\n#define AHEAD " << ahead << "\n#define ROW_TILES " << row_tiles << "\n#define EACH " << each << "\n#define STAGED " << (int)staged << "\n#define STEPS " << steps << "\n";
+  // (the parts of chunk c have groups c * parts and on where the row is a whole number of such runs: no run leaves its row then)
+  const bool spread = steps < 4 && (128 % G != 0 || groups % (4 / steps) != 0);
   // x's rows, and what they are a part of, begin on words' boundaries
   bool x_words = xa.offset % 2 == 0;
   for (int a : rows) x_words = x_words && stride_of(xa, a) % 2 == 0;
   k << "#define X_WORDS " << (int)(x_words || X.dtype == DNNF_F32) << "\n";
+  k << "#define TURNED " << (int)(steps < 4 || !staged) << "\n#define SPREAD " << (int)spread << "\n";
   k << "#define PX p0\n#define PW p1\n#define PS p2\n#define PZ p3\n";
   k << gemm_offset_fn(c, "offX_row", rows, xa) << gemm_offset_fn(c, "offX_batch", {}, xa);
   const std::string kparams = c.param_list(params, written);

@@ -258,6 +258,14 @@ def test_int4(dtype, M, K, N, G, zeros):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K,N,G", [(1, 160, 40, 32), (2, 320, 37, 64), (6, 480, 33, 96), (9, 1000, 70, 160), (5, 1344, 48, 192), (16, 224, 10300, 32), (16, 416, 10300, 96),
+                                     (6, 192, 5200, 64)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_int4_groups_that_fill_no_chunk(dtype, M, K, N, G, zeros):
+    check_int4(dg.int4_graph(dtype, (M,), K, N, G, zeros))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("lead", [(1, 1), (2, 3), (2, 2, 5)])
 def test_int4_with_what_follows_it(dtype, lead):
     check_int4(dg.int4_graph(dtype, lead, 160, 72, 32, True, bias=True))

@@ -151,17 +151,18 @@ DEV frag_t decode(const u32 w) {
   return __builtin_bit_cast(frag_t, r);
 }
 
-extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
+extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS SCRATCH) {
   __shared__ __attribute__((aligned(16))) float part[WAVES][ROWS][16 * NT + 1];
 #if STAGED
-  // x once per workgroup in the order of the codes (rows 16 bytes apart in their banks, zeros behind K)
-  __shared__ __attribute__((aligned(16))) part_t xs[XP][ROWS][CHUNKS * CHUNK + 8];
+  // its part of x once per workgroup in the order of the codes (rows 16 bytes apart in their banks, zeros behind K)
+  __shared__ __attribute__((aligned(16))) part_t xs[XP][ROWS][RANGE * CHUNK + 8];
 #endif
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, h = lane >> 4;
   // The tiles of one column range, which read the same weights, lie eight workgroups apart: on one die, one after another.
   const int group = blockIdx.x / (8 * ROW_TILES), member = blockIdx.x % (8 * ROW_TILES);
   const idx_t c0 = (idx_t)(group * 8 + member % 8) * (16 * NT), r0 = (idx_t)(member / 8) * 16;
   if (c0 >= GN) return;
+  const int base = SPLITS > 1 ? blockIdx.y * RANGE : 0;              // this workgroup's part of K, in chunks
   const unsigned char* __restrict__ wr[NT];
   const elem_t* __restrict__ sr[NT];
   const unsigned char* __restrict__ zr[NT];
@@ -247,7 +248,7 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
         frag_t x[XP];
 #if STAGED
 #pragma unroll
-        for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(n, ROWS - 1)][k];
+        for (int q = 0; q < XP; ++q) x[q] = *(const frag_t*)&xs[q][min(n, ROWS - 1)][k - base * CHUNK];
 #else
         load_x(xr, k, x, reach);
 #endif
@@ -274,15 +275,15 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
   };
 
   // this wavefront's chunks: EACH successive ones, so that it reads runs of EACH * 64 bytes of a row; AHEAD of them on their way
-  const int first = wave * EACH, last = min(first + EACH, CHUNKS);
+  const int first = base + wave * EACH, last = min(first + EACH, min(base + RANGE, CHUNKS));
   run_t ring[AHEAD];
 #pragma unroll
   for (int p = 0; p < AHEAD; ++p) load(ring[p], max(min(first + p, last - 1), 0));
 #if STAGED
-  for (int i = tid; i < ROWS * (CHUNKS * 16); i += 64 * WAVES) {
-    const int r = i / (CHUNKS * 16), k = i % (CHUNKS * 16) * 8;
+  for (int i = tid; i < ROWS * (RANGE * 16); i += 64 * WAVES) {
+    const int r = i / (RANGE * 16), k = i % (RANGE * 16) * 8;
     frag_t x[XP];
-    load_x(PX + offX_batch(0) + offX_row(min(r0 + r, (idx_t)(GM - 1))), k, x, cut_t());
+    load_x(PX + offX_batch(0) + offX_row(min(r0 + r, (idx_t)(GM - 1))), base * CHUNK + k, x, cut_t());
 #pragma unroll
     for (int q = 0; q < XP; ++q) *(frag_t*)&xs[q][r][k] = x[q];
   }
@@ -312,10 +313,30 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void KNAME(KPARAMS) {
     float v = part[0][rl][cl];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) v += part[w][rl][cl];
+#if SPLITS > 1
+    scratch[((idx_t)blockIdx.y * GM + r0 + rl) * GN + c0 + cl] = v;
+#else
     float cv[NCOLV > 0 ? NCOLV : 1];
     col_loads(c0 + cl, cv, KARGS);
     epilogue(0, r0 + rl, c0 + cl, v, cv, KARGS);
+#endif
   }
+}
+)KRN";
+
+// the sums of the parts of K, joined
+const char* kInt4JoinBody = R"KRN(
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS SCRATCH) {
+  const idx_t at = (idx_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= (idx_t)GM * GN) return;
+  float part[SPLITS], v = 0.0f;
+#pragma unroll
+  for (int i = 0; i < SPLITS; ++i) part[i] = scratch[(idx_t)i * GM * GN + at];
+#pragma unroll
+  for (int i = 0; i < SPLITS; ++i) v += part[i];
+  float cv[NCOLV > 0 ? NCOLV : 1];
+  col_loads(at % GN, cv, KARGS);
+  epilogue(0, at / GN, at % GN, v, cv, KARGS);
 }
 )KRN";
 
@@ -395,10 +416,18 @@ Lowered lower_int4(LowerCtx& c) {
   // would be 64 workgroups: 11.0 and 7.0).  Two or four row tiles a wavefront, for one pass over the codes, were no faster (64 rows,
   // 4096 x 4096: 20.9 and 22.6 us).
   const int64_t row_tiles = (M + 15) / 16, chunks = (K + 127) / 128, xp = X.dtype == DNNF_F32 ? 3 : 1;
-  const bool staged = xp * M <= 4 && xp * M * (chunks * 128 + 8) * 2 <= 40 * 1024;
+  // Few tiles of a long contraction: K is split among workgroups too, a chunk or more a wavefront, as far as the compute units go, and a
+  // second kernel (2 us) joins the sums: 2 rows, 32000 x 1024: 10.3 us, 29.8 in one; 4 rows, 8896 x 841: 6.9 and 10.5; 16 rows,
+  // 8320 x 1024: 6.8 and 12.0.  More than one workgroup a unit, or shorter K, gains nothing (one row, 4096 x 4096: 6.7 us, 4.1 in
+  // one; 16 rows, 11008 x 4096: 21.4 and 17.2; 16 rows, 4096 x 1024: 7.1 and 7.1).
+  const int64_t tiles = (N + 15) / 16 * row_tiles;
+  int64_t splits = tiles <= 128 && chunks > (xp * M <= 4 ? 64 : 32) ? std::min<int64_t>({256 / tiles, (chunks + 15) / 16, 32}) : 1;
+  const int64_t range = (chunks + splits - 1) / splits;
+  splits = (chunks + range - 1) / range;
+  const bool staged = xp * M <= 4 && xp * M * (range * 128 + 8) * 2 <= 40 * 1024;
   int64_t NT = 4;
   while (NT > 1 && (N + 16 * NT - 1) / (16 * NT) * row_tiles < (staged ? 512 : 160)) NT /= 2;
-  const int64_t most = std::min<int64_t>(16, chunks), each = (chunks + most - 1) / most, waves = (chunks + each - 1) / each, ahead = std::min<int64_t>(each, 2);
+  const int64_t most = std::min<int64_t>(16, range), each = (range + most - 1) / most, waves = (range + each - 1) / each, ahead = std::min<int64_t>(each, 2);
   const int steps = G % 128 == 0 || G >= K ? 4 : G % 64 == 0 ? 2 : 1;
 
   std::ostringstream k;
@@ -421,25 +450,35 @@ Lowered lower_int4(LowerCtx& c) {
   std::string kargs;
   for (size_t i = 0; i < params.size(); i++) kargs += (i ? ", p" : "p") + std::to_string(i);
   k << gemm_epilogue_source(c, {}, rows, cols, pslot, kparams, N, -1);
-  k << "#define KPARAMS " << kparams << "\n#define KARGS " << kargs << "\n" << kInt4Body;
+  k << "#define KPARAMS " << kparams << "\n#define KARGS " << kargs << "\n#define SPLITS " << splits << "\n#define RANGE " << range << "\n";
+  k << "#define SCRATCH " << (splits > 1 ? ", float* __restrict__ scratch" : "") << "\n";
 
   Lowered L;
   L.family = FAM_INT4;
   L.ext_in.assign(params.begin(), params.begin() + n_in);
   L.ext_out.assign(params.begin() + n_in, params.end());
-  Launch Kn;
-  Kn.params = params;
   const int64_t blocks = ((N + 16 * NT - 1) / (16 * NT) + 7) / 8 * 8 * row_tiles;
   DNNF_CHECK(blocks < (int64_t)1 << 31, DNNF_UNSUPPORTED_OP, "MatMulInt4: more workgroups than one launch takes");
-  Kn.grid[0] = (unsigned)blocks;
-  Kn.block[0] = (unsigned)(64 * waves);
-  std::string src = std::string(device_preamble()) + k.str();
-  Kn.name = fnv_name("dnnf_int4", src);
-  size_t pos;
-  while ((pos = src.find("KNAME")) != std::string::npos) src.replace(pos, 5, Kn.name);
-  Kn.source = src;
-  L.launches.push_back(Kn);
-  L.variant = "int4_16x" + std::to_string(16 * NT) + "_w" + std::to_string(waves) + "_g" + std::to_string(32 * steps);
+  auto launch = [&](const char* stem, const char* body, int64_t gx, int64_t gy, int64_t threads) {
+    Launch Kn;
+    Kn.params = params;
+    Kn.grid[0] = (unsigned)gx;
+    Kn.grid[1] = (unsigned)gy;
+    Kn.block[0] = (unsigned)threads;
+    Kn.scratch = splits > 1;
+    std::string src = std::string(device_preamble()) + k.str() + body;
+    Kn.name = fnv_name(stem, src);
+    size_t pos;
+    while ((pos = src.find("KNAME")) != std::string::npos) src.replace(pos, 5, Kn.name);
+    Kn.source = src;
+    L.launches.push_back(Kn);
+  };
+  launch("dnnf_int4", kInt4Body, blocks, splits, 64 * waves);
+  if (splits > 1) {
+    L.scratch_bytes = splits * M * N * 4;
+    launch("dnnf_int4_join", kInt4JoinBody, (M * N + 255) / 256, 1, 256);
+  }
+  L.variant = "int4_16x" + std::to_string(16 * NT) + "_w" + std::to_string(waves) + "_g" + std::to_string(32 * steps) + (splits > 1 ? "_k" + std::to_string(splits) : "");
   return L;
 }
 

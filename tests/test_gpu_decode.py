@@ -266,6 +266,12 @@ def test_int4_groups_that_fill_no_chunk(dtype, M, K, N, G, zeros):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K,N,G", [(1, 8320, 41, 128), (2, 8801, 24, 96), (20, 10947, 151, 128), (5, 16400, 17, 64), (1, 70000, 1, 32), (130, 8330, 100, 160)])
+def test_int4_long_contractions_into_few_columns(dtype, M, K, N, G):
+    check_int4(dg.int4_graph(dtype, (M,), K, N, G, True, bias=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("lead", [(1, 1), (2, 3), (2, 2, 5)])
 def test_int4_with_what_follows_it(dtype, lead):
     check_int4(dg.int4_graph(dtype, lead, 160, 72, 32, True, bias=True))

@@ -1031,8 +1031,10 @@ Lowered lower_block(const Graph& g, const Block& b, const LowerOpts& o) {
   DNNF_CHECK(anchors <= 1 || (attention && anchors == 3) || (gemm_norm && anchors == 2) || (se_tail && anchors == n_conv + n_gap), DNNF_UNSUPPORTED_OP,
              "a block may hold one Many-to-Many operator");
   Lowered L;
-  // a lone contiguous Reorganize operator moves nothing: its output shares the input's storage
+  // a lone contiguous Reorganize operator moves nothing: its output shares the input's storage (unless a Cast was merged into
+  // it: then it converts)
   if (b.ops.size() == 1 && g.ops[b.ops[0]].info->cls == OC_RESHAPE &&
+      g.tensors[g.ops[b.ops[0]].out[0]].dtype == g.tensors[g.ops[b.ops[0]].in[0]].dtype &&
       g.tensors[g.ops[b.ops[0]].out[0]].kind == DNNF_INTERMEDIATE && g.tensors[g.ops[b.ops[0]].in[0]].perm.empty() &&
       g.tensors[g.ops[b.ops[0]].out[0]].perm.empty()) {
     L.family = FAM_ALIAS;

@@ -81,3 +81,61 @@ def int4_graph(dtype, lead, K, N, G, zeros=False, bias=False, seed=5):
         y = b.op("Relu", [b.op("Add", [y, b.weight("bias", (N,), normal(seed, 6, (N,), dtype))], tuple(lead) + (N,))], tuple(lead) + (N,))
     b.mark_output(y)
     return b.finish()
+
+
+def cast_graph(how):
+    """A Cast between float types with a Reshape between it and an operator that fixes its operands' types."""
+    b = GraphBuilder("cast_" + how, "f32")
+    f16 = dict(out_dtype="f16")
+    if how == "attend_reshape_cast":           # fp32 results, reshaped, narrowed, multiplied in float16
+        b.g = attend_graph("f32", "i8", [9, 40])
+        y = b.op("Cast", [b.op("Reshape", ["o"], (2, 256), {"shape": [2, 256]})], (2, 256), {"to": 10}, **f16)
+        b.g.tensors["o"].kind = "intermediate"
+        y = b.op("MatMul", [y, b.weight("proj", (256, 32), normal(7, 7, (256, 32), "f16", 0.1), dtype="f16")], (2, 32), **f16)
+    elif how == "cast_reshape_attend":         # float16 queries, widened, reshaped, attended with in fp32
+        b.g = attend_graph("f32", "i8", [9, 40])
+        x = b.input("x", (512,), normal(7, 7, (512,), "f16"), dtype="f16")
+        b.g.ops[0].inputs[0] = b.op("Reshape", [b.op("Cast", [x], (512,), {"to": 1})], (2, 4, 64), {"shape": [2, 4, 64]})
+        del b.g.tensors["q"]
+        y = "o"
+    elif how == "cast_reshape_int4":
+        b.g = int4_graph("f32", (3,), 96, 40, 32, True)
+        x = b.input("x16", (288,), normal(7, 7, (288,), "f16"), dtype="f16")
+        b.g.ops[0].inputs[0] = b.op("Reshape", [b.op("Cast", [x], (288,), {"to": 1})], (3, 96), {"shape": [3, 96]})
+        del b.g.tensors["x"]
+        y = b.g.ops[0].outputs[0]
+    elif how == "int4_reshape_cast":
+        b.g = int4_graph("f32", (3,), 96, 40, 32, True)
+        y = b.g.ops[0].outputs[0]
+        b.g.tensors[y].kind = "intermediate"
+        y = b.op("Cast", [b.op("Reshape", [y], (120,), {"shape": [120]})], (120,), {"to": 10}, **f16)
+    elif how == "write_and_read":              # new rows widened and reshaped, the cache's contents reshaped and narrowed
+        b.g = write_graph("f32", "f32", 5, [0, 6])
+        for n in "kv":
+            x = b.input(n + "16", (640,), normal(7, ord(n), (640,), "f16"), dtype="f16")
+            b.g.ops[0].inputs[2 + "kv".index(n)] = b.op("Reshape", [b.op("Cast", [x], (640,), {"to": 1})], (2, 5, 2, 32), {"shape": [2, 5, 2, 32]})
+            del b.g.tensors[n]
+        kept, held = b.g.ops[0].outputs, b.input("held", (2,), np.array([5, 11]), dtype="i32")
+        write = b.g.ops.pop(0)
+        b.g.ops.append(write)
+        rows = [b._add(n + "_all", "f32", (2, 12, 2, 32), "intermediate") for n in "kv"]
+        b.g.ops.append(OpSpec("CacheRead", kept + ["table", held], rows, {"length": 12}))
+        for r in rows:
+            y = b.op("Relu", [b.op("Cast", [b.op("Reshape", [r], (24, 64), {"shape": [24, 64]})], (24, 64), {"to": 10}, **f16)], (24, 64), **f16)
+            b.mark_output(y)
+    else:                                      # ordinary operators: widened, reshaped, and a product in fp32
+        x = b.input("x", (288,), normal(7, 7, (288,), "f16"), dtype="f16")
+        y = b.op("Reshape", [b.op("Cast", [x], (288,), {"to": 1})], (3, 96), {"shape": [3, 96]})
+        y = b.op("MatMul", [y, b.weight("proj", (96, 32), normal(7, 8, (96, 32), "f32", 0.1))], (3, 32))
+    b.mark_output(y)
+    order, done = [], {n for n, t in b.g.tensors.items() if t.kind in ("input", "weight")}
+    while len(order) < len(b.g.ops):           # operators behind what they read
+        for op in b.g.ops:
+            if op not in order and all(i in done for i in op.inputs):
+                order.append(op)
+                done.update(op.outputs)
+    b.g.ops = order
+    return b.finish()
+
+
+CASTS = ("attend_reshape_cast", "cast_reshape_attend", "cast_reshape_int4", "int4_reshape_cast", "write_and_read", "cast_reshape_matmul")

@@ -534,3 +534,23 @@ def test_static_workspace():
     s.outputs[0][0].zero_()
     s.plan.run_static(s.in_ptrs(), s.out_ptrs(), s.stream)
     np.testing.assert_array_equal(s.result()["o"], got["o"])
+
+
+# ------------------------------------------------------------------------------------------------ types on the way
+@pytest.mark.parametrize("how", dg.CASTS)
+@pytest.mark.parametrize("fusion", [0, 1])
+def test_casts_behind_reshapes(how, fusion):
+    """Casts that the rewriting merges into a Reshape next to operators of another type: rows of the cache to half a step of
+    float16 (the written pools exactly), the other results to parity's bound of 16 bits - bytes read as another type are off by
+    the values' own size."""
+    from parity import TOL, rel_err
+
+    spec = dg.cast_graph(how)
+    _, got = run(spec, fusion=fusion)
+    for n, w in run_graph(spec).items():
+        if n.endswith("_new"):
+            np.testing.assert_array_equal(got[n], w, err_msg=n)
+        elif how == "write_and_read":
+            assert np.all(np.abs(got[n] - w) <= np.maximum(dg.HALF_STEP["f16"] * np.abs(w), 2.0 ** -25)), n
+        else:
+            assert rel_err(got[n], w) <= TOL["f16"], n

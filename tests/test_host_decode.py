@@ -272,3 +272,14 @@ def test_host_code_under_sanitizers(tmp_path):
     assert r.returncode == 0, (r.stdout[-2000:], r.stderr[-6000:])
     assert "Sanitizer" not in r.stderr and "runtime error" not in r.stderr, r.stderr[-6000:]
     assert r.stdout.count("\nok ") + r.stdout.startswith("ok ") == len(files), r.stdout
+
+
+# ------------------------------------------------------------------------------------------------ storage that is shared
+@pytest.mark.parametrize("how", dg.CASTS)
+@pytest.mark.parametrize("fusion", [0, 1])
+def test_storage_is_shared_between_tensors_of_one_type_only(how, fusion):
+    """A Cast behind or in front of a Reshape is merged into it by the rewriting: that Reshape converts, and shares nothing."""
+    p = plan(dg.cast_graph(how), fusion=fusion)
+    for b in p.dump_json()["blocks"]:
+        if api.FAMILY_NAMES[b["family"]] == "alias":
+            assert len({t["dtype"] for t in b["inputs"] + b["outputs"]}) == 1, b

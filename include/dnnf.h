@@ -108,8 +108,8 @@ dnnf_status dnnf_graph_set_const(dnnf_graph* g, int tensor_id, const double* val
  *   CacheWrite (k_pool, v_pool, [k_scale, v_scale,] k, v, table, first [, count]) -> k_pool, v_pool [, k_scale, v_scale]
  *       Token t of sequence b in k, v [B, T, HK, channels] becomes position first[b] + t, for t below count[b] (an operand that may
  *       be left out: T); positions below 0 or behind the table's M * S are left out.  The pools are INPUT tensors, updated in
- *       place: the results are OUTPUT tensors that take the same pointers at run time (anything else is refused), and other
- *       operators read the results.  All other rows stay as they are.  A slot written twice in one call keeps the last row
+ *       place: the results are OUTPUT tensors that take the same pointers at run time, each pool of the graph a buffer of its own
+ *       (anything else is refused before a call launches anything), and other operators read the results.  All other rows stay as they are.  A slot written twice in one call keeps the last row
  *       (by sequence, then by token).
  *   CacheRead (k_pool, v_pool, [k_scale, v_scale,] table, held) -> k, v     attribute "length" = L
  *       Positions 0 .. L - 1 laid out as [B, L, HK, channels]; zeros from held[b] on and where no page is.

@@ -421,6 +421,7 @@ dnnf_status dnnf_plan_run_static(dnnf_plan* p, const void* const* in, void* cons
 dnnf_status dnnf_plan_run_block(dnnf_plan* p, int b, const void* const* in, void* const* out, void* ws, void* stream) {
   return guard([&] {
     REQUIRE(p && b >= 0 && b < (int)p->p->blocks.size(), "bad block index");
+    p->p->check_buffers((size_t)b, (size_t)b + 1, in, out, ws);
     p->p->launch_block((size_t)b, in, out, ws, stream);
   });
 }

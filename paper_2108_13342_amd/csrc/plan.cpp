@@ -231,16 +231,33 @@ void* Plan::resolve(int t, const void* const* in, void* const* out, void* ws) co
   return (char*)ws + ws_offset[t] + within;
 }
 
+void Plan::check_buffers(size_t first, size_t last, const void* const* in, void* const* out, void* ws) const {
+  struct Range { const char* at; const char* end; int tensor; };
+  std::vector<Range> updated;
+  for (size_t b = first; b < last; b++)
+    for (auto& pr : blocks[b].low.in_place) {
+      const Tensor &R = g.tensors[pr.first], &X = g.tensors[pr.second];
+      const char* at = (const char*)resolve(pr.second, in, out, ws);
+      DNNF_CHECK(out && out[R.ext_index] == at, DNNF_INVALID_ARG, "output " + R.name + " is input " + X.name + " updated in place: both take the same pointer");
+      updated.push_back({at, at + X.bytes(), pr.second});
+    }
+  if (updated.empty()) return;
+  std::sort(updated.begin(), updated.end(), [](const Range& x, const Range& y) { return x.at < y.at; });
+  for (size_t i = 1; i < updated.size(); i++)
+    DNNF_CHECK(updated[i].at >= updated[i - 1].end, DNNF_INVALID_ARG,
+               "two tensors that are updated in place share one buffer: " + g.tensors[updated[i - 1].tensor].name + " and " + g.tensors[updated[i].tensor].name);
+  // (a missing pointer is found here and not between two launches)
+  for (size_t b = first; b < last; b++)
+    if (!blocks[b].blk.weight_only)
+      for (auto& L : blocks[b].low.launches) {
+        for (int t : L.params) (void)resolve(t, in, out, ws);
+        DNNF_CHECK(ws || !L.scratch, DNNF_INVALID_ARG, "workspace pointer is null");
+      }
+}
+
 void Plan::launch_block(size_t b, const void* const* in, void* const* out, void* ws, void* stream) {
   PlanBlock& pb = blocks[b];
   DNNF_CHECK(pb.low.family >= 0, DNNF_UNSUPPORTED_OP, "block has no kernel (plan was built for analysis only): " + pb.low.variant);
-  for (size_t i = 0; i < pb.low.in_place.size(); i++) {
-    const Tensor &R = g.tensors[pb.low.in_place[i].first], &X = g.tensors[pb.low.in_place[i].second];
-    const void* at = resolve(pb.low.in_place[i].second, in, out, ws);
-    DNNF_CHECK(out && out[R.ext_index] == at, DNNF_INVALID_ARG, "output " + R.name + " is input " + X.name + " updated in place: both take the same pointer");
-    for (size_t j = 0; j < i; j++)
-      DNNF_CHECK(resolve(pb.low.in_place[j].second, in, out, ws) != at, DNNF_INVALID_ARG, "two tensors that are updated in place share one buffer: " + X.name);
-  }
   for (size_t li = 0; li < pb.low.launches.size(); li++) {
     const Launch& L = pb.low.launches[li];
     if (pb.fn.size() <= li) pb.fn.resize(pb.low.launches.size(), nullptr);
@@ -371,6 +388,7 @@ void Plan::run_static(const void* const* in, void* const* out, void* stream) {
       DNNF_CHECK(pb.fn.size() > li && pb.fn[li], DNNF_NOT_FINALIZED,
                  "the plan's kernels are not resident: call dnnf_plan_prepare once (a null workspace is enough) before dnnf_plan_run_static");
   }
+  check_buffers(0, blocks.size(), in, out, slot.ptr);
   if (slot.owner != serial) {
     // another plan (or nobody) used the array last: its contents are that plan's.  Compiler-made constants and the
     // results of the weight-only blocks are put back; everything else is written by this run before it is read.
@@ -405,7 +423,7 @@ void Plan::run(const void* const* in, void* const* out, void* ws, void* stream) 
     for (size_t b = 0; b < blocks.size(); b++)
       if (!blocks[b].blk.weight_only) launch_block(b, in, out, ws, s);
   };
-  if (!use_graphs) { plain(stream); return; }
+  if (!use_graphs) { check_buffers(0, blocks.size(), in, out, ws); plain(stream); return; }
   std::vector<const void*> key;
   for (size_t i = 0; i < g.inputs.size(); i++) key.push_back(in ? in[i] : nullptr);
   for (size_t i = 0; i < g.outputs.size(); i++) key.push_back(out ? out[i] : nullptr);
@@ -413,6 +431,7 @@ void Plan::run(const void* const* in, void* const* out, void* ws, void* stream) 
   RunGraph* rg = nullptr;
   for (auto& e : impl->graphs) if (e.key == key) rg = &e;
   if (rg && rg->exec) { HIP_OK(hipGraphLaunch(rg->exec, (hipStream_t)stream)); return; }
+  check_buffers(0, blocks.size(), in, out, ws);
   if (!rg) {
     if (impl->graphs.size() >= 16) {       // callers that never repeat a buffer set gain nothing: stop trying
       use_graphs = false;
@@ -450,6 +469,7 @@ void Plan::run(const void* const* in, void* const* out, void* ws, void* stream) 
 }
 
 double Plan::time_block(size_t b, const void* const* in, void* const* out, void* ws, void* stream, int warmup, int iters) {
+  check_buffers(b, b + 1, in, out, ws);
   hipEvent_t e0, e1;
   HIP_OK(hipEventCreate(&e0));
   HIP_OK(hipEventCreate(&e1));

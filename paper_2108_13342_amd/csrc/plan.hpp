@@ -43,6 +43,9 @@ struct Plan {
   void layout_workspace();
   void* resolve(int tensor, const void* const* in, void* const* out, void* ws) const;
   void* function_for(const Launch& L);
+  // Before the first launch of a call: what the blocks update in place is given as input and as output, each in a buffer of its
+  // own, and every pointer is there.  A call that is refused has changed nothing.
+  void check_buffers(size_t first, size_t last, const void* const* in, void* const* out, void* ws) const;
   void launch_block(size_t b, const void* const* in, void* const* out, void* ws, void* stream);
   void load_kernels();             // every code object of the plan resident on the current device
   void prepare(void* ws, void* stream);

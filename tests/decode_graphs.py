@@ -139,3 +139,15 @@ def cast_graph(how):
 
 
 CASTS = ("attend_reshape_cast", "cast_reshape_attend", "cast_reshape_int4", "int4_reshape_cast", "write_and_read", "cast_reshape_matmul")
+
+
+def two_caches_graph():
+    """Two layers' caches, written one after the other in one graph."""
+    b = GraphBuilder("two_caches", "f16")
+    table, P = pages_of(5, 2, 4)
+    t, first = b.input("table", table.shape, table, dtype="i32"), b.input("first", (2,), np.array([0, 3]), dtype="i32")
+    for layer in range(2):
+        pools = [b.input(f"{n}_pool{layer}", (P, 2, 8, 32), normal(6, 2 * layer + i, (P, 2, 8, 32), "f16")) for i, n in enumerate("kv")]
+        new = [b.input(f"{n}{layer}", (2, 3, 2, 32), normal(7, 2 * layer + i, (2, 3, 2, 32), "f16")) for i, n in enumerate("kv")]
+        b.g.ops.append(OpSpec("CacheWrite", pools + new + [t, first], [b._add(p + "_new", "f16", b.shape(p), "output") for p in pools]))
+    return b.finish()

@@ -554,3 +554,30 @@ def test_casts_behind_reshapes(how, fusion):
             assert np.all(np.abs(got[n] - w) <= np.maximum(dg.HALF_STEP["f16"] * np.abs(w), 2.0 ** -25)), n
         else:
             assert rel_err(got[n], w) <= TOL["f16"], n
+
+
+@pytest.mark.parametrize("graphs", [0, 1])
+def test_a_refused_call_leaves_the_caches_alone(graphs):
+    """The second layer's pointers are wrong: the first layer's pools are as they were.  The right call still works afterwards."""
+    import torch
+
+    from paper_2108_13342_amd import api
+
+    spec = dg.two_caches_graph()
+    s = api.Session(spec, graphs=graphs)
+    ins, outs = s.in_ptrs(), s.out_ptrs()
+    before = [t.clone() for t in s.outputs[0]]
+    spare = torch.zeros_like(before[3])
+    at = [t.name for t in spec.inputs()].index("v_pool1")
+    for i, o in ((ins, outs[:3] + [spare.data_ptr()]), (ins[:at] + [outs[0]] + ins[at + 1:], outs[:3] + [outs[0]])):
+        with pytest.raises(api.DnnfError):
+            s.plan.run(i, o, s.workspace.data_ptr(), s.stream)
+        with pytest.raises(api.DnnfError):
+            s.plan.run_static(i, o, s.stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(before, s.outputs[0]))
+    for _ in range(3):
+        s.run()
+    got = s.result()
+    for n, w in run_graph(spec).items():
+        np.testing.assert_array_equal(got[n], w, err_msg=n)

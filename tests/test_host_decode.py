@@ -283,3 +283,29 @@ def test_storage_is_shared_between_tensors_of_one_type_only(how, fusion):
     for b in p.dump_json()["blocks"]:
         if api.FAMILY_NAMES[b["family"]] == "alias":
             assert len({t["dtype"] for t in b["inputs"] + b["outputs"]}) == 1, b
+
+
+@pytest.mark.parametrize("graphs", [0, 1])
+def test_buffers_are_looked_at_before_anything_is_launched(graphs):
+    """Two layers' caches.  Nothing is at these addresses, and there is no GPU: a refusal of the second layer's buffers comes before
+    the first layer's kernel is so much as loaded."""
+    spec = dg.two_caches_graph()
+    p = plan(spec, graphs=graphs)
+    names = [t.name for t in spec.inputs()]
+    at = {n: (i + 1) << 20 for i, n in enumerate(names)}
+    outs = [at[t.name.replace("_new", "")] for t in spec.outputs()]
+
+    def call(match, ins=(), out=()):
+        a = [dict(ins).get(n, at[n]) for n in names]
+        o = [dict(out).get(t.name, x) for t, x in zip(spec.outputs(), outs)]
+        for run in (lambda: p.run(a, o, 1 << 30), lambda: p.bind(a, o, 1 << 30).run()):
+            with pytest.raises(api.DnnfError, match=match) as e:
+                run()
+            assert e.value.code == INVALID
+
+    call("v_pool1_new is input v_pool1 updated in place", out=[("v_pool1_new", 12345 << 4)])
+    call("v_pool1_new", out=[("v_pool1_new", 0)])
+    call("missing input pointer for k1", ins=[("k1", 0)])
+    for other in ("k_pool0", "v_pool0", "k_pool1"):      # two pools in one buffer, or in buffers that overlap
+        for off in (0, 64, -64):
+            call("share one buffer", ins=[("v_pool1", at[other] + off)], out=[("v_pool1_new", at[other] + off)])

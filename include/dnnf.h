@@ -110,7 +110,8 @@ dnnf_status dnnf_graph_set_const(dnnf_graph* g, int tensor_id, const double* val
  *       be left out: T); positions below 0 or behind the table's M * S are left out.  The pools are INPUT tensors, updated in
  *       place: the results are OUTPUT tensors that take the same pointers at run time, each pool of the graph a buffer of its own
  *       (anything else is refused before a call launches anything), and other operators read the results.  All other rows stay as they are.  A slot written twice in one call keeps the last row
- *       (by sequence, then by token).
+ *       (by sequence, then by token).  A call of many pages (B * ((T + S - 2) / S + 1) above 4096) takes 4 bytes of workspace for
+ *       every slot of a pool.
  *   CacheRead (k_pool, v_pool, [k_scale, v_scale,] table, held) -> k, v     attribute "length" = L
  *       Positions 0 .. L - 1 laid out as [B, L, HK, channels]; zeros from held[b] on and where no page is.
  *   CacheAttention (q, k_pool, v_pool, [k_scale, v_scale,] table, held) -> o     attributes "scale", "window"

@@ -22,25 +22,19 @@ namespace dnnf {
 namespace {
 
 // ------------------------------------------------------------------------------------------------ CacheWrite
-const char* kWriteBody = R"KRN(
+// Pages of all sequences together that a call may write and still have every workgroup look through them: the work is their
+// square, in rounds of 256.  Above, three kernels whose work is the tokens'.  Looked through and settled first, twelve heads of 64
+// channels, bfloat16: one token of 2048 sequences 4.8 and 10.4 us; in pages of 16, 32 x 1024 tokens (2080 pages) 32.2 and 33.8, 64 x 1024
+// 87.3 and 88.0, 64 x 2048 179 and 167.  51 x 3525 tokens of one head of 32 channels in pages of one slot would be 1.2e10 looks: 16.7 us.
+constexpr int64_t kSearchedPages = 4096;
+
+// Rows of new keys and values on their way into the pools: LANES lanes a row.
+const char* kWriteRows = R"KRN(
 #define VEC (16 / (int)sizeof(elem_t))
 #define VECTORS(D) ((D) / VEC)
+#define NEW(seq) (HAS_COUNT ? count[seq] : TOKENS)
 typedef elem_t in_t __attribute__((ext_vector_type(VEC)));
 typedef pool_t out_t __attribute__((ext_vector_type(VEC)));
-
-// positions [lo, hi) that a sequence writes whose operands are `f` and `n`
-DEV void written(const int f, const int n, int& lo, int& hi) {
-  lo = min(max(f, 0), TABLE * SLOTS);
-  hi = (int)min((long long)f + min(max(n, 0), TOKENS), (long long)TABLE * SLOTS);
-}
-// the page that entry e of all sequences' written pages lies in, whose first position is p0; -1: nothing is written there
-DEV int written_page(const int e, const int f, const int n, const int* __restrict__ table, int& lo, int& hi, int& p0) {
-  written(f, n, lo, hi);
-  const int lp = min(lo / SLOTS + e % SPANS, TABLE - 1);
-  const int page = table[(long long)(e / SPANS) * TABLE + lp];
-  p0 = lp * SLOTS;
-  return lo < hi && p0 < hi && lp == lo / SLOTS + e % SPANS ? page : -1;
-}
 
 template <int D> DEV in_t take(const elem_t* __restrict__ x, const long long src, const int lane) {
   in_t v = 0;
@@ -100,18 +94,38 @@ template <int D> DEV void put(pool_t* __restrict__ pool, float* __restrict__ sca
   if (on) *(out_t*)(pool + dst * D + lane * VEC) = v;
 #endif
 }
+)KRN";
+
+const char* kWriteBody = R"KRN(
+// positions [lo, hi) that a sequence writes whose operands are `f` and `n`
+DEV void written(const int f, const int n, int& lo, int& hi) {
+  lo = min(max(f, 0), TABLE * SLOTS);
+  hi = (int)min((long long)f + min(max(n, 0), TOKENS), (long long)TABLE * SLOTS);
+}
+// the page that entry e of all sequences' written pages lies in, whose first position is p0; -1: nothing is written there
+DEV int written_page(const int e, const int f, const int n, const int* __restrict__ table, int& lo, int& hi, int& p0) {
+  written(f, n, lo, hi);
+  const int lp = min(lo / SLOTS + e % SPANS, TABLE - 1);
+  const int page = table[(long long)(e / SPANS) * TABLE + lp];
+  p0 = lp * SLOTS;
+  return lo < hi && p0 < hi && lp == lo / SLOTS + e % SPANS ? page : -1;
+}
+// which of the CHUNK slots from s0 on are among positions [lo, hi) of a page whose first position is p0
+DEV u32 slots_of(const int lo, const int hi, const int p0, const int s0) {
+  const int a = max(lo - p0 - s0, 0), z = min(hi - p0 - s0, CHUNK);
+  return a < z ? (1u << z) - (1u << a) : 0u;
+}
 
 // Bound by memory for long prompts (8 x up to 2048 tokens of eight heads of 128 channels, float16 to 8 bits: 78 MB in 22 us; 4 x up to
 // 1024 tokens of twelve heads of 64, bfloat16: 20 MB in 3.6 us), by the chain of loads - numbers, pages, rows - for a few
 // (2.3 us for one token of four sequences, 5.3 us for 2 x 37 tokens to 8 bits).
 // A workgroup writes CHUNK positions that lie in one page, for HEADS_EACH heads; LANES lanes a row.  Where one slot is written
 // twice in a call the last write stays (sequences in order, then tokens): a workgroup looks through the written pages behind
-// its own for the same page - once, and row by row only if there is one.
+// its own for its slots, 256 pages at a time.
 extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
-  __shared__ int clash;
+  __shared__ u32 clash;                                          // bit i: the i-th of this workgroup's positions is written again
   const int tid = threadIdx.x, unit = blockIdx.x, head0 = blockIdx.y * HEADS_EACH;
   const int entry = unit / SUBS, b = entry / SPANS;
-#define NEW(seq) (HAS_COUNT ? count[seq] : TOKENS)
   // (of the entry that this thread looks through as well: two rounds of loads in all, the numbers and then pages and rows)
   const int other = entry + 1 + tid, ob = min(other, SEQUENCES * SPANS - 1) / SPANS, f = first[b], n = NEW(b), of = first[ob], on = NEW(ob);
   int lo, hi;
@@ -132,27 +146,80 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
     vx[i] = take<DV>(v, src, lane);
   }
   int l, h, q;
-  bool same = written_page(min(other, SEQUENCES * SPANS - 1), of, on, table, l, h, q) == page && other < SEQUENCES * SPANS;
+  u32 later = written_page(min(other, SEQUENCES * SPANS - 1), of, on, table, l, h, q) == page && other < SEQUENCES * SPANS ? slots_of(l, h, q, p0 % SLOTS) : 0u;
   if ((u32)page >= (u32)PAGES) return;
   if (tid == 0) clash = 0;
   __syncthreads();
-  for (int e = other + 256; e < SEQUENCES * SPANS; e += 256) same |= written_page(e, first[e / SPANS], NEW(e / SPANS), table, l, h, q) == page;
-  if (same) clash = 1;
+  for (int e = other + 256; e < SEQUENCES * SPANS; e += 256)
+    if (written_page(e, first[e / SPANS], NEW(e / SPANS), table, l, h, q) == page) later |= slots_of(l, h, q, p0 % SLOTS);
+  if (later) atomicOr(&clash, later);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int r = tid / LANES + i * (256 / LANES), p = p0 + r / HEADS_EACH, head = head0 + r % HEADS_EACH;
-    if (r >= rows || head >= HEADS) continue;
-    if (clash) {
-      bool later = false;
-      for (int e = entry + 1; e < SEQUENCES * SPANS && !later; ++e) {
-        if (written_page(e, first[e / SPANS], NEW(e / SPANS), table, l, h, q) == page) later = q + p % SLOTS >= l && q + p % SLOTS < h;
-      }
-      if (later) continue;
-    }
+    if (r >= rows || head >= HEADS || (clash >> (p - p0) & 1u)) continue;
     const long long dst = ((long long)page * HEADS + head) * SLOTS + p % SLOTS;
     put<DK>(k_pool, k_scale, kx[i], dst, lane);
     put<DV>(v_pool, v_scale, vx[i], dst, lane);
+  }
+}
+)KRN";
+
+// The same for calls that write many pages, where looking through all of them from every workgroup would be work in the square of
+// their number.  Which token has a slot is settled first, in an array with a place for every slot of the pool, by two kernels over the
+// tokens: each token stores its number in its slot's place, then numbers above the stored one are raised into it.  Every place that
+// counts has been stored to by a token of this call, so the array needs no clearing, and the largest number, the last
+// token, stays whatever the order.
+const char* kWriteClaimBody = R"KRN(
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  const u32 i = blockIdx.x * 256u + threadIdx.x, b = i / TOKENS;
+  if (b >= SEQUENCES) return;
+  const int t = (int)(i % TOKENS);
+  const long long p = (long long)first[b] + t;
+  if (t >= NEW(b) || p < 0 || p >= TABLE * SLOTS) return;
+  const int page = table[(long long)b * TABLE + (int)p / SLOTS];
+  if ((u32)page >= (u32)PAGES) return;
+  u32* __restrict__ own = owner + ((long long)page * SLOTS + (int)p % SLOTS);
+#if RAISE
+  if (__hip_atomic_load(own, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < i) __hip_atomic_fetch_max(own, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#else
+  __hip_atomic_store(own, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#endif
+}
+)KRN";
+
+// The rows of the tokens that their slots belong to; a row wherever it lies, so that pages of any size fill the workgroups.
+const char* kWriteOwnedBody = R"KRN(
+extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
+  const int lane = threadIdx.x % LANES;
+  const idx_t base = (idx_t)blockIdx.x * (256 / LANES * PASSES) + threadIdx.x / LANES;
+  in_t kx[PASSES], vx[PASSES];
+  long long dst[PASSES];
+  bool mine[PASSES];
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const idx_t r = base + i * (256 / LANES);
+    mine[i] = false;
+    dst[i] = 0;
+    kx[i] = 0;
+    vx[i] = 0;
+    if (r >= (idx_t)SEQUENCES * TOKENS * HEADS) continue;
+    const idx_t token = r / HEADS;
+    const int b = (int)(token / TOKENS), t = (int)(token % TOKENS);
+    const long long p = (long long)first[b] + t;
+    if (t >= NEW(b) || p < 0 || p >= TABLE * SLOTS) continue;
+    kx[i] = take<DK>(k, r, lane);
+    vx[i] = take<DV>(v, r, lane);
+    const int page = table[(long long)b * TABLE + (int)p / SLOTS];
+    if ((u32)page >= (u32)PAGES) continue;
+    mine[i] = owner[(long long)page * SLOTS + (int)p % SLOTS] == (u32)token;
+    dst[i] = ((long long)page * HEADS + (int)(r % HEADS)) * SLOTS + (int)p % SLOTS;
+  }
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    if (!mine[i]) continue;
+    put<DK>(k_pool, k_scale, kx[i], dst[i], lane);
+    put<DV>(v_pool, v_scale, vx[i], dst[i], lane);
   }
 }
 )KRN";
@@ -735,21 +802,39 @@ Lowered lower_cache(LowerCtx& c) {
     const int64_t spans = (o.T + o.S - 2) / o.S + 1, subs = (o.S + chunk - 1) / chunk;
     int64_t lanes = 1;
     while (lanes * vec < std::max(o.D[0], o.D[1])) lanes *= 2;
+    const int64_t at_once = 256 / lanes;
+    k << "typedef " << elem << " elem_t;\n#define ELEM_BYTES " << 16 / vec << "\n#define TOKENS " << o.T << "\n#define LANES " << lanes << "\n#define HAS_COUNT " << (int)(o.count >= 0) << "\n";
+    if (o.count < 0) k << "#define count ((const int*)0)\n";
+    const std::string where = std::string("const int* __restrict__ table, const int* __restrict__ first") + (o.count >= 0 ? ", const int* __restrict__ count" : "");
+    const std::string rows = "pool_t* __restrict__ k_pool, pool_t* __restrict__ v_pool" + scales(true) + ", const elem_t* __restrict__ k, const elem_t* __restrict__ v, " + where;
+    params = op.out;
+    params.push_back(o.fresh[0]);
+    params.push_back(o.fresh[1]);
+    std::vector<int> where_params = {o.table, o.first};
+    if (o.count >= 0) where_params.push_back(o.count);
+    params.insert(params.end(), where_params.begin(), where_params.end());
+    for (size_t i = 0; i < op.out.size(); i++) L.in_place.push_back({op.out[i], op.in[i]});
+    if (o.B * spans > kSearchedPages) {
+      DNNF_CHECK(o.B <= (((int64_t)1 << 32) - 256) / o.T, DNNF_UNSUPPORTED_OP, "CacheWrite: 2^32 tokens or more in one call");
+      const int64_t total = o.B * o.T * o.HK, passes = 4;
+      k << "#define PASSES " << passes << "\ntypedef " << (total < ((int64_t)1 << 31) - at_once * passes ? "int" : "long long") << " idx_t;\n";
+      for (int raise = 0; raise < 2; raise++)
+        L.launches.push_back(make_launch("dnnf_cache_claim", k.str() + "#define RAISE " + std::to_string(raise) + "\n#define NEW(seq) (HAS_COUNT ? count[seq] : TOKENS)\n#define KPARAMS " + where +
+                                         ", u32* __restrict__ owner\n", kWriteClaimBody, where_params, (o.B * o.T + 255) / 256));
+      L.launches.push_back(make_launch("dnnf_cache_write", k.str() + "#define KPARAMS " + rows + ", const u32* __restrict__ owner\n" + kWriteRows, kWriteOwnedBody, params,
+                                       (total + at_once * passes - 1) / (at_once * passes)));
+      for (auto& launch : L.launches) launch.scratch = true;
+      L.scratch_bytes = o.P * o.S * 4;
+      L.variant = std::string("cache_write_owned") + (o.eight_bits ? "_i8" : "");
+      return L;
+    }
     // rows a lane: four where that leaves two workgroups per compute unit, else two or one (4 x 1024 tokens of twelve heads of 64
     // channels: 3.9 us; 7.6 with all heads of sixteen tokens in a workgroup)
-    const int64_t at_once = 256 / lanes, tokens = std::min(chunk, o.T), passes_of = o.B * o.T * o.HK / at_once;
+    const int64_t tokens = std::min(chunk, o.T), passes_of = o.B * o.T * o.HK / at_once;
     const int64_t want = passes_of >= 4 * 512 ? 4 : passes_of >= 2 * 512 ? 2 : 1;
     const int64_t heads = std::min(o.HK, std::max<int64_t>(1, want * at_once / tokens)), passes = (tokens * heads + at_once - 1) / at_once;
-    DNNF_CHECK(o.B * spans < (int64_t)1 << 30, DNNF_UNSUPPORTED_OP, "CacheWrite: too many pages in one call");
-    k << "typedef " << elem << " elem_t;\n#define ELEM_BYTES " << 16 / vec << "\n#define TOKENS " << o.T << "\n#define SPANS " << spans << "\n#define SUBS " << subs << "\n#define CHUNK " << chunk
-      << "\n#define LANES " << lanes << "\n#define HEADS_EACH " << heads << "\n#define PASSES " << passes << "\n#define HAS_COUNT " << (int)(o.count >= 0) << "\n";
-    if (o.count < 0) k << "#define count ((const int*)0)\n";
-    k << "#define KPARAMS pool_t* __restrict__ k_pool, pool_t* __restrict__ v_pool" << scales(true) << ", const elem_t* __restrict__ k, const elem_t* __restrict__ v, "
-      << "const int* __restrict__ table, const int* __restrict__ first" << (o.count >= 0 ? ", const int* __restrict__ count" : "") << "\n";
-    params = op.out;
-    for (int t : {o.fresh[0], o.fresh[1], o.table, o.first}) params.push_back(t);
-    if (o.count >= 0) params.push_back(o.count);
-    for (size_t i = 0; i < op.out.size(); i++) L.in_place.push_back({op.out[i], op.in[i]});
+    k << "#define SPANS " << spans << "\n#define SUBS " << subs << "\n#define CHUNK " << chunk << "\n#define HEADS_EACH " << heads << "\n#define PASSES " << passes << "\n";
+    k << "#define KPARAMS " << rows << "\n" << kWriteRows;
     L.launches.push_back(make_launch("dnnf_cache_write", k.str(), kWriteBody, params, o.B * spans * subs));
     L.launches[0].grid[1] = (unsigned)((o.HK + heads - 1) / heads);
     DNNF_CHECK(L.launches[0].grid[1] < 65536, DNNF_UNSUPPORTED_OP, "CacheWrite: too many heads");

@@ -581,3 +581,37 @@ def test_a_refused_call_leaves_the_caches_alone(graphs):
     got = s.result()
     for n, w in run_graph(spec).items():
         np.testing.assert_array_equal(got[n], w, err_msg=n)
+
+
+# ------------------------------------------------------------------------------------------------ many pages in one call
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("T,S,M,first,count", [
+    (1400, 1, 1500, [0, 150, -9], [1400, 1400, 1400]),                       # the second runs off its table, the third begins before its own
+    (1400, 1, 1400, [0, 2147483647, -2147483648], None),
+    (2801, 2, 1410, [1, 7, 0], [2801, 0, -3]),
+    (2800, 2, 1401, [0, 0, 1], [2147483647, 1, 2800]),
+])
+def test_write_many_pages(dtype, cache, T, S, M, first, count):
+    spec = dg.write_graph(dtype, cache, T, first, count, S=S, M=M, DK=48, DV=16, HK=3)
+    s, _ = run(spec)
+    assert "owned" in s.plan.describe()[0]["kernel_name"]
+    check_written(spec)
+
+
+@pytest.mark.parametrize("B,T,S,M", [(2, 2200, 1, 2200), (700, 4, 4, 2), (2100, 4, 4, 2), (1400, 1, 16, 1), (40, 30, 1, 30)])
+@pytest.mark.parametrize("cache", ["f16", "i8"])
+def test_a_slot_written_many_times_keeps_the_last(B, T, S, M, cache):
+    """Tables of few pages, so that most slots are written over and over, some entries not there: on both sides of the number of
+    pages up to which workgroups look through them, and replayed."""
+    P = 60
+    table = dg.rng.integers(9, 1, (B, M), -2, P + 2)
+    first = dg.rng.integers(9, 2, (B,), -1, 2 * S)
+    count = dg.rng.integers(9, 3, (B,), T // 2, T + 2)
+    spec = dg.write_graph("f16", cache, T, first, count, S=S, M=M, table=table, P=P, DK=16, DV=32)
+    s, got = run(spec)
+    want = run_graph(spec)
+    for _ in range(3):
+        for n, w in want.items():
+            np.testing.assert_array_equal(got[n], w, err_msg=n)
+        s.run()
+        got = s.result()

@@ -309,3 +309,14 @@ def test_buffers_are_looked_at_before_anything_is_launched(graphs):
     for other in ("k_pool0", "v_pool0", "k_pool1"):      # two pools in one buffer, or in buffers that overlap
         for off in (0, 64, -64):
             call("share one buffer", ins=[("v_pool1", at[other] + off)], out=[("v_pool1_new", at[other] + off)])
+
+
+def test_writing_many_pages_is_no_square_of_work():
+    """Up to 4096 pages a call every workgroup looks through them all; above, three kernels settle who writes a slot."""
+    few = plan(dg.write_graph("f16", "f16", 2048, [0, 0], S=1, M=2048)).describe()[0]
+    assert few["n_kernel_launches"] == 1 and "cache_write_chunk1" in few["kernel_name"]
+    p = plan(dg.write_graph("f16", "i8", 2049, [0, 0], S=1, M=2049))
+    assert p.describe()[0]["n_kernel_launches"] == 3 and "cache_write_owned_i8" in p.describe()[0]["kernel_name"]
+    pages = 2 * 2049 + 3
+    assert p.workspace_bytes() >= 4 * pages      # a place for every slot of the pool
+    p.precompile()

@@ -119,7 +119,8 @@ DEV u32 slots_of(const int lo, const int hi, const int p0, const int s0) {
 // Bound by memory for long prompts (8 x up to 2048 tokens of eight heads of 128 channels, float16 to 8 bits: 78 MB in 22 us; 4 x up to
 // 1024 tokens of twelve heads of 64, bfloat16: 20 MB in 3.6 us), by the chain of loads - numbers, pages, rows - for a few
 // (2.3 us for one token of four sequences, 5.3 us for 2 x 37 tokens to 8 bits).
-// A workgroup writes CHUNK positions that lie in one page, for HEADS_EACH heads; LANES lanes a row.  Where one slot is written
+// A workgroup writes CHUNK positions that lie in one page, counted from the first written one there (a page may hold a whole
+// sequence: its other slots need no workgroups), for HEADS_EACH heads; LANES lanes a row.  Where one slot is written
 // twice in a call the last write stays (sequences in order, then tokens): a workgroup looks through the written pages behind
 // its own for its slots, 256 pages at a time.
 extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
@@ -133,7 +134,7 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
   if (lo >= hi) return;
   const int lp = lo / SLOTS + entry % SPANS;
   if (lp >= TABLE) return;
-  const int p0 = max(lo, lp * SLOTS + unit % SUBS * CHUNK), p1 = min(hi, min(lp * SLOTS + (unit % SUBS + 1) * CHUNK, (lp + 1) * SLOTS));
+  const int p0 = max(lo, lp * SLOTS) + unit % SUBS * CHUNK, p1 = min(hi, min(p0 + CHUNK, (lp + 1) * SLOTS));
   if (p0 >= p1) return;
   const int page = table[(long long)b * TABLE + lp];
   const int lane = tid % LANES, rows = (p1 - p0) * HEADS_EACH;
@@ -799,7 +800,7 @@ Lowered lower_cache(LowerCtx& c) {
   if (cls == OC_CACHE_WRITE) {
     const std::string elem = c.ctype(g.tensors[o.fresh[0]].dtype);
     const int64_t vec = 16 / dtype_bytes(g.tensors[o.fresh[0]].dtype), chunk = std::min<int64_t>(o.S, 16);
-    const int64_t spans = (o.T + o.S - 2) / o.S + 1, subs = (o.S + chunk - 1) / chunk;
+    const int64_t spans = (o.T + o.S - 2) / o.S + 1, subs = (std::min(o.S, o.T) + chunk - 1) / chunk;
     int64_t lanes = 1;
     while (lanes * vec < std::max(o.D[0], o.D[1])) lanes *= 2;
     const int64_t at_once = 256 / lanes;

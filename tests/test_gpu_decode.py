@@ -615,3 +615,12 @@ def test_a_slot_written_many_times_keeps_the_last(B, T, S, M, cache):
             np.testing.assert_array_equal(got[n], w, err_msg=n)
         s.run()
         got = s.result()
+
+
+@pytest.mark.parametrize("T,S,M,first,count", [(1, 300, 1, [0, 299, 150, 300], None), (37, 300, 2, [290, 0, 263, 599], None), (37, 100, 3, [-9, 95, 64, 250], [37, 20, 36, 37]),
+                                               (300, 128, 3, [1, 127, 100, 200], [300, 300, 17, 150])])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "i8")])
+def test_write_into_large_pages(dtype, cache, T, S, M, first, count):
+    check_written(dg.write_graph(dtype, cache, T, first, count, S=S, M=M))
+    table = np.array([[0] * M, [1] * M, [0] * M, [0] * M])      # and where three sequences share a page
+    check_written(dg.write_graph(dtype, cache, T, first, count, S=S, M=M, table=table, P=2))

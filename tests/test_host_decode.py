@@ -320,3 +320,15 @@ def test_writing_many_pages_is_no_square_of_work():
     pages = 2 * 2049 + 3
     assert p.workspace_bytes() >= 4 * pages      # a place for every slot of the pool
     p.precompile()
+
+
+def test_writing_into_a_large_page_takes_workgroups_for_its_tokens_only():
+    for T, S, most in ((1, 1 << 17, 2 * 1), (40, 1 << 17, 2 * 2 * 3), (40, 64, 2 * 2 * 3), (64, 64, 2 * 2 * 4), (1 << 10, 64, 2 * 17 * 4)):
+        g = api.Graph()
+        pools = [g.add_tensor(n, "f16", (2, 1, S, 16), "input") for n in "kv"]
+        new = [g.add_tensor(n + "n", "f16", (2, T, 1, 16), "input") for n in "kv"]
+        at = [g.add_tensor("table", "i32", (2, 16), "input"), g.add_tensor("first", "i32", (2,), "input")]
+        g.add_op("CacheWrite", pools + new + at, [g.add_tensor(n + "o", "f16", (2, 1, S, 16), "output") for n in "kv"])
+        g.finalize()
+        grid = api.Plan(g, []).dump_json()["blocks"][0]["launches"][0]["grid"]
+        assert grid[0] <= most and grid[1] == 1, (T, S, grid)

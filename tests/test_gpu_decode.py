@@ -624,3 +624,32 @@ def test_write_into_large_pages(dtype, cache, T, S, M, first, count):
     check_written(dg.write_graph(dtype, cache, T, first, count, S=S, M=M))
     table = np.array([[0] * M, [1] * M, [0] * M, [0] * M])      # and where three sequences share a page
     check_written(dg.write_graph(dtype, cache, T, first, count, S=S, M=M, table=table, P=2))
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("DK", [64, 80])
+def test_queries_with_infinities(dtype, cache, DK):
+    """Scores of -infinity alone give zeros, +infinity and NaN among them NaN, and the other heads' results stay as they were."""
+    spec = dg.attend_graph(dtype, cache, [150, 40], HQ=6, HK=1, DK=DK, DV=32, S=16, M=10)
+    q, k = (np.array(spec.tensors[n].data, dtype=np.float64) for n in ("q", "k_pool"))
+    k[..., 3] = np.where(k[..., 3] == 0, 1, np.abs(k[..., 3]))          # channel 3 above zero in all keys, 5 in all but one held one
+    k[..., 5] = np.where(k[..., 5] == 0, 1, np.abs(k[..., 5]))
+    table = spec.tensors["table"].data
+    k[table[0, 4], :, 2, 5] = -1
+    k[..., 70 % DK] = np.where(k[..., 70 % DK] == 0, 1, np.abs(k[..., 70 % DK]))
+    k[table[0, 4], :, 2, 9] = 0
+    spec.tensors["k_pool"].data = k
+    spec.tensors["q"].data = q
+    want = run(spec)[1]["o"]
+    q = np.array(q)
+    q[0, 0, 3] = -np.inf                 # -infinity everywhere
+    q[0, 1, 5] = -np.inf                 # +infinity once
+    q[0, 2, 9] = np.inf                  # infinity times zero once
+    q[0, 3, [3, 70 % DK]] = -np.inf      # two channels, of one sign
+    q[1, 4, 40] = np.nan
+    spec.tensors["q"].data = q
+    got = run(spec)[1]["o"]
+    assert np.all(got[0, [0, 3]] == 0.0)
+    assert np.all(np.isnan(got[0, 1])) and np.all(np.isnan(got[0, 2])) and np.all(np.isnan(got[1, 4]))
+    np.testing.assert_array_equal(got[0, 4:], want[0, 4:])
+    np.testing.assert_array_equal(got[1, [0, 1, 2, 3, 5]], want[1, [0, 1, 2, 3, 5]])

@@ -251,7 +251,8 @@ typedef struct {
                               attention (opts.attention), 7 squeeze-excite tail (opts.squeeze_excite),
                               8 key / value cache (CacheWrite, CacheRead, CacheAttention), 9 MFMA product with weights of
                               four bits (MatMulInt4) */
-  double bytes;            /* algorithmic HBM bytes: external inputs read once + outputs written once */
+  double bytes;            /* algorithmic HBM bytes: external inputs read once + outputs written once; of a pool the rows that the
+                              operator writes or its table, window or length reach at most, not all pages (flops likewise) */
   double flops;
   double irs_bytes_removed;/* intermediate results that never reach HBM (Table 5's IRS statistic) */
   int n_kernel_launches;

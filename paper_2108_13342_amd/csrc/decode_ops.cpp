@@ -1,5 +1,7 @@
 // Operands, shapes and checks of the operators of single-token inference: a key / value cache kept in pages (CacheWrite,
 // CacheRead, CacheAttention) and products with weights of four bits (MatMulInt4).
+#include <algorithm>
+
 #include "ir.hpp"
 
 namespace dnnf {
@@ -73,6 +75,25 @@ CacheOperands cache_operands(const Graph& g, const Op& op) {
     agree(c.HK >= 1 && c.HQ >= 1 && c.HQ % c.HK == 0, "the query heads are no multiple of the key heads");
   }
   return c;
+}
+
+int64_t cache_positions(const Op& op, const CacheOperands& c) {
+  if (op.info->cls == OC_CACHE_WRITE) return std::min(c.T, c.M * c.S);
+  if (op.info->cls == OC_CACHE_READ) return std::min(c.T, c.M * c.S);
+  const int64_t window = whole_attr(op, "window");
+  return window > 0 ? std::min(window, c.M * c.S) : c.M * c.S;
+}
+
+double cache_bytes(const Graph& g, const Op& op) {
+  const CacheOperands c = cache_operands(g, op);
+  // (sequences may share pages, whose rows are then read once)
+  const int64_t all = c.B * cache_positions(op, c), rows = op.info->cls == OC_CACHE_WRITE ? all : std::min(all, c.P * c.S);
+  double bytes = (double)(rows * c.HK) * (double)((c.D[0] + c.D[1]) * dtype_bytes(g.tensors[c.pool[0]].dtype) + (c.eight_bits ? 8 : 0));
+  for (int t : {c.q, c.fresh[0], c.fresh[1], c.table, c.first, c.count, c.held})
+    if (t >= 0) bytes += (double)g.tensors[t].bytes();
+  if (op.info->cls != OC_CACHE_WRITE)
+    for (int t : op.out) bytes += (double)g.tensors[t].bytes();
+  return bytes;
 }
 
 Dims infer_decode_shape(const Graph& g, const Op& op, int oi) {

@@ -527,9 +527,9 @@ double op_flops(const Graph& g, const Op& op) {
       return 2.0 * on * (double)(op.i("transA", 0) ? a[0] : a[1]);
     }
     case OC_MATMUL_INT4: return 2.0 * on * (double)g.tensors[op.in[0]].dims.back();
-    case OC_CACHE_ATTN: {        // at the table's capacity (how many keys a sequence holds is known when it runs)
+    case OC_CACHE_ATTN: {        // at the table's capacity or the window (how many keys a sequence holds is known when it runs)
       const CacheOperands c = cache_operands(g, op);
-      return 2.0 * (double)(c.B * c.HQ) * (double)(c.M * c.S) * (double)(c.D[0] + c.D[1]);
+      return 2.0 * (double)(c.B * c.HQ) * (double)cache_positions(op, c) * (double)(c.D[0] + c.D[1]);
     }
     default: {
       double tot = 0;

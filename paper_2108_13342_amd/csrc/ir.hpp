@@ -169,6 +169,8 @@ struct CacheOperands {
 bool is_decode_op(const Op& op);
 CacheOperands cache_operands(const Graph& g, const Op& op);
 Dims infer_decode_shape(const Graph& g, const Op& op, int out_index);
+int64_t cache_positions(const Op& op, const CacheOperands& c);      // positions of a sequence that are written or read at most
+double cache_bytes(const Graph& g, const Op& op);        // what a cache operator reads and writes at most: rows, not whole pools
 void check_decode_op(const Graph& g, const Op& op);      // types, attributes, and what may share storage (a relinked graph)
 Dims broadcast_dims(const Dims& a, const Dims& b);
 int classify_op(const Graph& g, const Op& op);      // Table 2 + most-complex-pair rule

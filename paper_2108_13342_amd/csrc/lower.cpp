@@ -1196,6 +1196,7 @@ Lowered lower_block(const Graph& g, const Block& b, const LowerOpts& o) {
   L.bytes = 0;
   for (int t : ein) L.bytes += (double)g.tensors[t].bytes();
   for (int t : eout) L.bytes += (double)g.tensors[t].bytes();
+  if (L.family == FAM_CACHE) L.bytes = cache_bytes(g, g.ops[b.ops[0]]);
   L.flops = 0;
   for (int oi : b.ops) L.flops += g.ops[oi].flops;
   L.irs_removed = 0;

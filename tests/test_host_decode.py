@@ -332,3 +332,21 @@ def test_writing_into_a_large_page_takes_workgroups_for_its_tokens_only():
         g.finalize()
         grid = api.Plan(g, []).dump_json()["blocks"][0]["launches"][0]["grid"]
         assert grid[0] <= most and grid[1] == 1, (T, S, grid)
+
+
+def test_bytes_and_operations_are_of_the_rows_that_are_reached():
+    """A pool far larger than what its operators touch: counted is what the tables and attributes reach, rows once."""
+    def block(spec):
+        d = plan(spec).describe()[0]
+        return d["bytes"], d["flops"]
+
+    # 2 sequences, 3 tokens, 2 heads of 32 + 32 channels: rows in, rows out, tables and positions
+    assert block(dg.write_graph("f16", "f16", 3, [0, 9], P=5000))[0] == 2 * (2 * 3 * 2 * 64 * 2) + 4 * (2 * 6 + 2)
+    assert block(dg.write_graph("f32", "i8", 3, [0, 9], [1, 2], P=5000))[0] == 2 * 3 * 2 * (64 * 4 + 64 + 8) + 4 * (2 * 6 + 2 + 2)
+    assert block(dg.read_graph("f16", "i8", [5, 9], 10))[0] == 2 * 10 * 2 * (64 + 8 + 64 * 2) + 4 * (2 * 6 + 2)
+    assert block(dg.read_graph("f16", "f16", [5], 60, table=[[0, 1]]))[0] == 16 * 2 * 64 * 2 + 60 * 2 * 64 * 2 + 4 * (2 + 1)
+    # 2 x 128 positions, 2 key heads and 4 query heads of 64 + 64 channels
+    assert block(dg.attend_graph("bf16", "bf16", [9, 9], P=5000)) == (2 * 128 * 2 * 128 * 2 + 2 * 4 * 128 * 2 + 4 * (16 + 2), 2.0 * 2 * 4 * 128 * 128)
+    assert block(dg.attend_graph("bf16", "i8", [9, 9], P=5000, attrs={"window": 10})) == (2 * 10 * 2 * (128 + 8) + 2 * 4 * 128 * 2 + 4 * (16 + 2), 2.0 * 2 * 4 * 10 * 128)
+    # two sequences on one page
+    assert block(dg.attend_graph("bf16", "bf16", [9, 9], M=1, table=[[0], [0]], P=1))[0] == 16 * 2 * 128 * 2 + 2 * 4 * 128 * 2 + 4 * (2 + 2)

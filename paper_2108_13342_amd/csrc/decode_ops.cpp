@@ -130,6 +130,8 @@ void check_decode_op(const Graph& g, const Op& op) {
     DNNF_CHECK(type(op.in[1]) == DNNF_U8 && (op.in.size() < 4 || type(op.in[3]) == DNNF_U8), DNNF_INVALID_ARG, "MatMulInt4: weights and zero points are U8");
     for (int t : {op.in[0], op.in[1], op.out[0]})
       for (int64_t d : g.tensors[t].dims) DNNF_CHECK(d >= 1, DNNF_SHAPE_MISMATCH, "MatMulInt4: empty operand");
+    // positions along K, up to the end of the chunk behind the last, are counted in 32 bits
+    DNNF_CHECK(g.tensors[op.in[0]].dims.back() < ((int64_t)1 << 31) - 256, DNNF_UNSUPPORTED_OP, "MatMulInt4: a contraction of 2^31 or more");
     return;
   }
   const CacheOperands c = cache_operands(g, op);

@@ -789,7 +789,8 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
 )KRN";
 
 Launch make_launch(const std::string& prefix, const std::string& head, const char* body, std::vector<int> params, int64_t blocks) {
-  DNNF_CHECK(blocks >= 1 && blocks < (int64_t)1 << 31, DNNF_UNSUPPORTED_OP, "cache operator: more workgroups than one launch takes");
+  // (a launch has fewer than 2^32 threads along an axis)
+  DNNF_CHECK(blocks >= 1 && blocks < ((int64_t)1 << 32) / 256, DNNF_UNSUPPORTED_OP, "cache operator: more workgroups than one launch takes");
   Launch L;
   std::string src = std::string(device_preamble()) + head + body;
   L.name = fnv_name(prefix, src);

@@ -403,8 +403,9 @@ Lowered lower_int4(LowerCtx& c) {
     written.insert(s.tensor);
   }
   bool wide = false;
-  for (int t : params) wide = wide || g.tensors[t].n() >= (int64_t)1 << 31;
-  wide = wide || M * N >= (int64_t)1 << 31;
+  const int64_t far = ((int64_t)1 << 31) - (1 << 16);      // (tiles reach up to 511 columns behind the last one, and 15 rows)
+  for (int t : params) wide = wide || g.tensors[t].n() >= far;
+  wide = wide || M * N >= far;
 
   // ---- tile: sixteen rows; K split among up to sixteen wavefronts.  A product of one row is over before a long loop could settle:
   // what counts is that all of its weights are asked for at once (11008 x 4096, bfloat16, one row: 9.6 us with sixteen
@@ -458,7 +459,7 @@ Lowered lower_int4(LowerCtx& c) {
   L.ext_in.assign(params.begin(), params.begin() + n_in);
   L.ext_out.assign(params.begin() + n_in, params.end());
   const int64_t blocks = ((N + 16 * NT - 1) / (16 * NT) + 7) / 8 * 8 * row_tiles;
-  DNNF_CHECK(blocks < (int64_t)1 << 31, DNNF_UNSUPPORTED_OP, "MatMulInt4: more workgroups than one launch takes");
+  DNNF_CHECK(blocks * 64 * waves < (int64_t)1 << 32, DNNF_UNSUPPORTED_OP, "MatMulInt4: more workgroups than one launch takes");
   auto launch = [&](const char* stem, const char* body, int64_t gx, int64_t gy, int64_t threads) {
     Launch Kn;
     Kn.params = params;

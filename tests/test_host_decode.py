@@ -350,3 +350,33 @@ def test_bytes_and_operations_are_of_the_rows_that_are_reached():
     assert block(dg.attend_graph("bf16", "i8", [9, 9], P=5000, attrs={"window": 10})) == (2 * 10 * 2 * (128 + 8) + 2 * 4 * 128 * 2 + 4 * (16 + 2), 2.0 * 2 * 4 * 10 * 128)
     # two sequences on one page
     assert block(dg.attend_graph("bf16", "bf16", [9, 9], M=1, table=[[0], [0]], P=1))[0] == 16 * 2 * 128 * 2 + 2 * 4 * 128 * 2 + 4 * (2 + 2)
+
+
+def test_products_and_launches_beyond_the_index_ranges():
+    def product(M, K, N, G=32):
+        g = api.Graph()
+        ins = [g.add_tensor("x", "f16", (M, K), "input"), g.add_tensor("w", "u8", (N, (K + 1) // 2), "weight"), g.add_tensor("s", "f16", (N, -(-K // G)), "weight")]
+        g.add_op("MatMulInt4", ins, [g.add_tensor("y", "f16", (M, N), "output")], {"group_size": G})
+        g.finalize()
+        return api.Plan(g, [1, 1]).block_source(0)
+
+    # a tile's last columns lie behind the last one: their numbers have to fit too
+    for M, N in ((1, (1 << 31) - 300), (1, 1 << 31)):
+        assert "typedef long long idx_t" in product(M, 2, N)
+    assert "typedef int idx_t" in product(1, 2, 1 << 30)
+    product(1, (1 << 31) - 257, 1)
+    for K in ((1 << 31) - 256, 1 << 31, 1 << 33):
+        with pytest.raises(api.DnnfError, match="contraction of 2\\^31") as e:
+            product(1, K, 1)
+        assert e.value.code == UNSUPPORTED
+    # 2^32 threads and more in a launch
+    with pytest.raises(api.DnnfError, match="more workgroups than one launch takes") as e:
+        product(1 << 30, 32, 64)
+    assert e.value.code == UNSUPPORTED
+    g = api.Graph()
+    pools = [g.add_tensor(n, "f16", (4, 16, 16, 16), "input") for n in "kv"]
+    ins = [g.add_tensor("q", "f16", (1 << 19, 16 * 64, 16), "input")] + pools + [g.add_tensor("t", "i32", (1 << 19, 1), "input"), g.add_tensor("h", "i32", (1 << 19,), "input")]
+    g.add_op("CacheAttention", ins, [g.add_tensor("o", "f16", (1 << 19, 16 * 64, 16), "output")])
+    g.finalize()
+    with pytest.raises(api.DnnfError, match="more workgroups than one launch takes"):
+        api.Plan(g, [])

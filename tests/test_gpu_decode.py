@@ -653,3 +653,39 @@ def test_queries_with_infinities(dtype, cache, DK):
     assert np.all(np.isnan(got[0, 1])) and np.all(np.isnan(got[0, 2])) and np.all(np.isnan(got[1, 4]))
     np.testing.assert_array_equal(got[0, 4:], want[0, 4:])
     np.testing.assert_array_equal(got[1, [0, 1, 2, 3, 5]], want[1, [0, 1, 2, 3, 5]])
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "i8"), ("f16", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("HQ,HK,DK,DV,S,M,held", [
+    (24, 1, 256, 256, 16, 40, [640, 129, 3]),        # more than 64 KiB of LDS to join in, a second half-filled tile of queries
+    (28, 4, 256, 128, 20, 7, [140, 77]),
+    (48, 3, 128, 256, 8, 20, [160, 0, 33]),
+])
+def test_attention_of_many_heads_over_wide_channels(dtype, cache, HQ, HK, DK, DV, S, M, held):
+    check_attention(dg.attend_graph(dtype, cache, held, HQ, HK, DK, DV, S, M))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_probabilities_keep_their_second_part(dtype):
+    """check_attention without the allowance for one rounding of the probabilities: given in two parts, each is off by the square of
+    half a step u (float16: or by half of its smallest number, 2^-25, where the row's largest is 1 or more).  Small scores and few keys,
+    so that this is what is left; the oracle with probabilities rounded once is outside the bound."""
+    u = dg.HALF_STEP[dtype]
+    spec = dg.attend_graph(dtype, dtype, [9, 16, 30], HQ=8, HK=2, DK=64, DV=256, S=16, M=2, q_std=0.1)
+    q, k, v, table = (data(spec, n) for n in ("q", "k_pool", "v_pool", "table"))
+    want, once, bound = (np.zeros((3, 8, 256)) for _ in range(3))
+    for b, held in enumerate([9, 16, 30]):
+        at = [(int(table[b, p // 16]), p % 16) for p in range(held)]
+        for h in range(8):
+            kk, vv = (np.stack([x[page, h // 4, slot] for page, slot in at]) for x in (k, v))
+            s = kk @ q[b, h] / 8
+            p = np.exp(s - s.max())
+            rounded = dg.rng.round_to(p, dtype).astype(np.float64)
+            want[b, h], once[b, h] = p @ vv / p.sum(), rounded @ vv / p.sum()
+            score = np.abs(kk * q[b, h]).sum(-1).max() / 8
+            c = u * u + 2.0 ** -24 * (2 * (64 + 8) * score + 16 + held)
+            bound[b, h] = u * np.abs(want[b, h]) * (1 + 2.0 ** -8) + c * (p @ np.abs(vv)) / p.sum() + 2.0 ** -25 * np.abs(vv).sum(0)
+    np.testing.assert_allclose(run_graph(spec)["o"], want, rtol=1e-9, atol=1e-12)
+    assert np.mean(np.abs(once - want) > bound) > 0.05
+    off = np.abs(run(spec)[1]["o"] - want) - bound
+    assert np.all(off <= 0), f"{off.max():.3e} over its bound"

@@ -689,3 +689,37 @@ def test_probabilities_keep_their_second_part(dtype):
     assert np.mean(np.abs(once - want) > bound) > 0.05
     off = np.abs(run(spec)[1]["o"] - want) - bound
     assert np.all(off <= 0), f"{off.max():.3e} over its bound"
+
+
+def test_many_pages_captured_and_replayed():
+    """The write of many pages in a captured graph: what a replay leaves depends on the buffers' contents at that time alone, not
+    on what earlier calls left in the workspace; eager work and other contents between the replays."""
+    import torch
+
+    from paper_2108_13342_amd import api
+
+    B, T, S, M, P = 2100, 2, 4, 2, 50
+    spec = dg.write_graph("f16", "i8", T, np.zeros(B, dtype=np.int64), S=S, M=M, table=np.zeros((B, M), dtype=np.int64), P=P, DK=16, DV=16, HK=1)
+    s = api.Session(spec)
+    bound = s.plan.bind(s.in_ptrs(), s.out_ptrs(), s.workspace.data_ptr())
+    at = {t.name: s.inputs[0][i] for i, t in enumerate(spec.inputs())}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        bound.run(side.cuda_stream)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            bound.run(torch.cuda.current_stream().cuda_stream)
+    for step in range(4):
+        spec.tensors["table"].data = dg.rng.integers(step, 1, (B, M), -1, P)
+        spec.tensors["first"].data = dg.rng.integers(step, 2, (B,), 0, 7)
+        for n in ("table", "first"):
+            at[n].copy_(torch.from_numpy(spec.tensors[n].data))
+        s.workspace.random_(0, 256)
+        for n in [t.name for t in spec.inputs() if "pool" in t.name or "scale" in t.name]:
+            at[n].copy_(torch.from_numpy(np.asarray(spec.tensors[n].data)))
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, w in run_graph(spec).items():
+            np.testing.assert_array_equal(s.result()[n], w, err_msg=f"{n}, replay {step}")

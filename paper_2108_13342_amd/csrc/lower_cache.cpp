@@ -116,9 +116,10 @@ DEV u32 slots_of(const int lo, const int hi, const int p0, const int s0) {
   return a < z ? (1u << z) - (1u << a) : 0u;
 }
 
-// Bound by memory for long prompts (8 x up to 2048 tokens of eight heads of 128 channels, float16 to 8 bits: 78 MB in 22 us; 4 x up to
-// 1024 tokens of twelve heads of 64, bfloat16: 20 MB in 3.6 us), by the chain of loads - numbers, pages, rows - for a few
-// (2.3 us for one token of four sequences, 5.3 us for 2 x 37 tokens to 8 bits).
+// Bound by memory for long prompts (4 x up to 1024 tokens of twelve heads of 64 channels, bfloat16: 20 MB in 5.1 us; 8 x 2048 of eight
+// heads of 128: 134 MB in 20.5 us), by the chain of loads - numbers, pages, rows - for a few (2.2 us for one token of four
+// sequences).  To 8 bits the quantising comes behind the loads: 2 x 37 tokens of twelve heads of 64 take 2.6 us in bfloat16 and 3.4 to
+// 8 bits (3.7 behind another kernel), 8 x 2048 tokens of eight heads of 128 22.6 us for 102 MB.
 // A workgroup writes CHUNK positions that lie in one page, counted from the first written one there (a page may hold a whole
 // sequence: its other slots need no workgroups), for HEADS_EACH heads; LANES lanes a row.  Where one slot is written
 // twice in a call the last write stays (sequences in order, then tokens): a workgroup looks through the written pages behind
@@ -281,13 +282,18 @@ extern "C" __global__ __launch_bounds__(256) void KNAME(KPARAMS) {
 
 // ------------------------------------------------------------------------------------------------ CacheAttention
 // For a query q of a head: o = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = q . k_j * scale * log2(e), over the keys j
-// that its sequence holds.  The keys are read once, for all query heads that share them; m may be any reference (see below).
+// that its sequence holds.  The keys are read once for up to sixteen query heads that share them; each further sixteen are a workgroup
+// of their own that reads them again, at the same time and so mostly from the caches (131072 keys of one head of 128 channels,
+// bfloat16: 21.2 us for 16 query heads, 21.6 for 24).  m may be any reference (see below).
 //
-// Bound by memory: one sequence of 131072 keys (eight key heads of 128 channels, bfloat16) takes 92.5 us for 537 MB, 5.8 TB/s of the
-// 5.9 that a plain reading kernel reaches; sixteen sequences of 1000 to 4001 keys 39.7 us for 174 MB, 64 of 512 to 2048 in
-// 8 bits 44.8 us for 174 MB - there the longest sequence is what the others wait for, and the first loads (numbers, pages, rows,
-// one behind another) are not hidden.  Dealing the steps of all sequences out evenly over the workgroups cost more in
-// sequences begun than it gave (43.5 -> 46 us and 47 -> 56 us with the joining).
+// Bound by memory: one sequence of 131072 keys (eight key heads of 128 channels, bfloat16) takes 92.7 us for 537 MB, 5.8 TB/s of the
+// 5.9 that a plain reading kernel reaches; sixteen sequences of 1000 to 4001 keys 39.6 us for 174 MB, 64 of 512 to 2048 in
+// 8 bits 45.2 us for 174 MB - each sequence is cut into the same number of splits, so the longest is what the others wait for,
+// and the first loads (numbers, pages, rows, one behind another) are not hidden.  Dealing the steps of all sequences out evenly over
+// the workgroups cost more in sequences begun than it gave (43.5 -> 46 us and 47 -> 56 us with the joining); splits of one length
+// for all sequences were not tried.  Elsewhere, a pass with the joining: 32768 keys of eight heads of 256 channels, bfloat16, 52.6 us
+// (5.1 TB/s), in fp32 127 us (4.2 TB/s); of 128 channels in fp32 53.0 us (5.1 TB/s); 131072 keys of one head 3.2 TB/s, the 128
+// splits being all of its workgroups.
 //
 // Four wavefronts, each with 32 keys per step.  S = K . Q^T by 16x16 MFMA: keys are the rows, the (up to 16) query heads of a
 // key head the columns, so that a lane holds eight scores of one query and the softmax needs two exchanges.  Those scores,
@@ -861,8 +867,9 @@ Lowered lower_cache(LowerCtx& c) {
       L.variant = std::string("cache_write_owned") + (o.eight_bits ? "_i8" : "");
       return L;
     }
-    // rows a lane: four where that leaves two workgroups per compute unit, else two or one (4 x 1024 tokens of twelve heads of 64
-    // channels: 3.9 us; 7.6 with all heads of sixteen tokens in a workgroup)
+    // rows a lane: four where that leaves two workgroups per compute unit, else two or one (against all heads of sixteen tokens in a
+    // workgroup: 4 x 1024 tokens of twelve heads of 64 channels, bfloat16, 5.2 and 5.1 us, to 8 bits 6.9 and 9.8; 2 x 512 of 32 heads
+    // of 128 6.6 and 10.5, to 8 bits 9.6 and 39.7)
     const int64_t tokens = std::min(chunk, o.T), passes_of = o.B * o.T * o.HK / at_once;
     const int64_t want = passes_of >= 4 * 512 ? 4 : passes_of >= 2 * 512 ? 2 : 1;
     const int64_t heads = std::min(o.HK, std::max<int64_t>(1, want * at_once / tokens)), passes = (tokens * heads + at_once - 1) / at_once;

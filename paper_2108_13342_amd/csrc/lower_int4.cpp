@@ -1,7 +1,8 @@
 // Products with weights of four bits: y[m, n] = sum_k x[m, k] * (code[n, k] - zero[n, k / G]) * scale[n, k / G], for the few rows of
 // single-token inference.  The block may hold One-to-One operators, Reshapes and Splits behind the product, as behind MatMul.
 //
-// What bounds it: the weights, half a byte each and read once; everything else has to stay out of their way.
+// What bounds it: the weights, half a byte each and read once; everything else has to stay out of their way.  (Sizes here are rows of x,
+// then K x N; groups of 128 with zero points, bfloat16, where nothing else is said.)
 //   - A code becomes an operand of the matrix units by two instructions for two codes: shifted into the mantissa of 16 it is the
 //     number 16 + code, exactly, in float16 and bfloat16 alike.  The product of a group is then taken as
 //     sum x (16 + code) - (16 + zero) sum x; the row sums of x come from the matrix units too (a column of ones), in the layout
@@ -18,8 +19,11 @@
 //     4096 x 11008 in groups of 96: 13.8 us, 39.5 with a load for every part.  (In groups of 32, 4096 x 4096, the vector takes 7.8 us, the
 //     exchanges 8.6.)
 //   - fp32 x is taken in three bfloat16 parts, which hold all of its 24 bits; weights are exact in either case.
-// One row of 4096 x 11008 (groups of 128, bfloat16): 23.6 MB in 8.7 us, 2.7 TB/s; 50257 x 768 for 16 rows 21.5 MB in 8.9 us.  A kernel that
-// only has to be launched takes 2 us, its first loads another 2, and the bytes 4; nothing of this overlaps in so short a run.
+// One row of 4096 x 11008: 23.6 MB in 8.8 us, 2.7 TB/s; 16 rows of 768 x 50257 without zero points 21.5 MB in 9.3 us.  A compute unit holds two
+// workgroups of sixteen wavefronts, and what does not fit the 512 places waits for a second round that begins with its loads
+// again: one row of 4096 x 4096 takes 4.1 us, x 8192 (512 workgroups) 6.5, x 8208 8.1, x 11008 8.8, x 12288 9.1.  With weights that come from
+// memory, not from the memory-side cache: 9.4 us for x 11008, 10.3 for the 16 rows.
+// From 17 rows on every tile of sixteen rows decodes the weights again: 4096 x 4096 takes 13.4 us for 64 rows, 94 for 512, 360 for 2048 (191 TFLOP/s).
 // The wavefronts of a workgroup share its columns and split K among them; sums are joined in LDS in a fixed order.
 #include <algorithm>
 #include <sstream>
@@ -408,14 +412,14 @@ Lowered lower_int4(LowerCtx& c) {
   wide = wide || M * N >= far;
 
   // ---- tile: sixteen rows; K split among up to sixteen wavefronts.  A product of one row is over before a long loop could settle:
-  // what counts is that all of its weights are asked for at once (11008 x 4096, bfloat16, one row: 9.6 us with sixteen
-  // wavefronts, 11.7 with eight, 14.3 with four).
-  // Up to four rows x goes through LDS (one row, 4096 x 11008: 10.0 us, 14.3 with x read by every wavefront for itself; sixteen rows,
-  // 50257 x 768: 12.3 and 9.5) and a workgroup takes as many columns as leave two of them per compute unit.  With more rows
+  // what counts is that all of its weights are asked for at once (one row with sixteen wavefronts, eight, four: 4096 x 4096 4.1 us, 5.9
+  // and 5.4; 4096 x 11008 8.9, 14.6 and 12.9; 11008 x 4096 9.2, 9.1 and 9.7).
+  // Up to four rows x goes through LDS (one row, 4096 x 11008: 8.8 us, 9.3 with x read by every wavefront for itself; sixteen rows,
+  // 768 x 50257: 11.7 and 9.3) and a workgroup takes as many columns as leave two of them per compute unit.  With more rows
   // it is x that the wavefronts wait for, and wide tiles read it less often: as many columns as leave 160 workgroups (16 rows,
-  // 11008 x 4096: 13.6 us with 64 columns, 18.5 with 16; 64 rows, 4096 x 4096: 11.8 and 22.3; but 16 rows, 4096 x 4096, where that
-  // would be 64 workgroups: 11.0 and 7.0).  Two or four row tiles a wavefront, for one pass over the codes, were no faster (64 rows,
-  // 4096 x 4096: 20.9 and 22.6 us).
+  // 4096 x 11008: 13.3 us with 64 columns, 18.6 with 16; 64 rows, 4096 x 4096: 13.4 and 24.2; but 16 rows, 4096 x 4096, where that
+  // would be 64 workgroups: 12.8 and 7.4, and 11008 x 4096: 39.4 and 17.3).  Without zero points each takes a tenth less.  Two or four
+  // row tiles a wavefront, for one pass over the codes, were no faster (64 rows, 4096 x 4096: 20.9 and 22.6 us).
   const int64_t row_tiles = (M + 15) / 16, chunks = (K + 127) / 128, xp = X.dtype == DNNF_F32 ? 3 : 1;
   // Few tiles of a long contraction: K is split among workgroups too, a chunk or more a wavefront, as far as the compute units go, and a
   // second kernel (2 us) joins the sums: 2 rows, 32000 x 1024: 10.3 us, 29.8 in one; 4 rows, 8896 x 841: 6.9 and 10.5; 16 rows,

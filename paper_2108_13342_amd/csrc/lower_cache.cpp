@@ -577,7 +577,7 @@ extern "C" __global__ __launch_bounds__(256, OCCUPANCY) void KNAME(KPARAMS) {
     for (int j = 0; j < 8; ++j) unit = fmaxf(unit, __builtin_fabsf(t.vs[j / 4][j % 4]));
     unit = fmaxf(unit, __shfl_xor(unit, 16, 64));
     unit = fmaxf(unit, __shfl_xor(unit, 32, 64));
-    const float per_unit = unit > 0.0f ? dn_rcp(unit) : 0.0f;
+    const float per_unit = unit >= 1.17549435e-38f ? dn_rcp(unit) : 0.0f;      // (below the normal numbers it would be infinite)
 #endif
     pfrag_t p[PN];
 #pragma unroll

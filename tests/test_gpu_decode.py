@@ -723,3 +723,20 @@ def test_many_pages_captured_and_replayed():
         torch.cuda.synchronize()
         for n, w in run_graph(spec).items():
             np.testing.assert_array_equal(s.result()[n], w, err_msg=f"{n}, replay {step}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_steps_below_the_normal_numbers(dtype):
+    """A cache of 8 bits that somebody else filled, some values' steps zero or below 2^-126, alone among their neighbours or not: such
+    rows are within 127 * 2^-126 of zero, and so is what they add."""
+    spec = dg.attend_graph(dtype, "i8", [100, 31, 64], S=16, M=8)
+    t, table = spec.tensors["v_scale"], spec.tensors["table"].data
+    t.data = np.array(t.data)
+    t.data[table[0, 2]] = 1e-40
+    t.data[table[0, 4], :, 3] = 2.0 ** -149
+    t.data[table[1, :]] = 1e-39
+    t.data[table[2, :2]] = 0.0
+    _, got = run(spec)
+    assert np.all(np.abs(got["o"][1]) <= 127 * 2.0 ** -126)
+    assert np.all(np.isfinite(got["o"]))
+    check_attention(spec, got)

@@ -109,24 +109,25 @@ dnnf_status dnnf_graph_set_const(dnnf_graph* g, int tensor_id, const double* val
  *       Token t of sequence b in k, v [B, T, HK, channels] becomes position first[b] + t, for t below count[b] (an operand that may
  *       be left out: T); positions below 0 or behind the table's M * S are left out.  The pools are INPUT tensors, updated in
  *       place: the results are OUTPUT tensors that take the same pointers at run time, each pool of the graph a buffer of its own
- *       (anything else is refused before a call launches anything), and other operators read the results.  All other rows stay as they are.  A slot written twice in one call keeps the last row
- *       (by sequence, then by token).  A call of many pages (B * ((T + S - 2) / S + 1) above 4096) takes 4 bytes of workspace for
- *       every slot of a pool.
+ *       (anything else is refused before a call launches anything), and other operators read the results.  All other rows stay as
+ *       they are.  A slot written twice in one call keeps the last row (by sequence, then by token).  A call of many pages
+ *       (B * ((T + S - 2) / S + 1) above 4096) takes 4 bytes of workspace for every slot of a pool.
  *   CacheRead (k_pool, v_pool, [k_scale, v_scale,] table, held) -> k, v     attribute "length" = L
  *       Positions 0 .. L - 1 laid out as [B, L, HK, channels]; zeros from held[b] on and where no page is.
  *   CacheAttention (q, k_pool, v_pool, [k_scale, v_scale,] table, held) -> o     attributes "scale", "window"
  *       One new token per sequence: q [B, HQ, channels of a key] -> [B, HQ, channels of a value], HQ a multiple of HK (query head
  *       h reads key head h / (HQ / HK)).  Softmax(scale q K^T) V over positions 0 .. held[b] - 1 (the last "window" of them if that
  *       is above 0); scale is 1 / sqrt(channels of a key) unless given.  Without any key, or with scores of -infinity alone, the
- *       result is zeros.  held is taken within [0, M * S].  Slots that are not read may hold anything, NaN included.
+ *       result is zeros.  held is taken within [0, M * S].  Slots that are not read may hold anything, NaN included; a channel of the
+ *       values that are read with an infinity or NaN in it comes out as an infinity or NaN, not always the one of the formula.
  * q, k, v and o are of the pools' type, of any float type if the pools are I8.
  *
  *   MatMulInt4 (x, w, scale [, zero]) -> y     attribute "group_size" = G, a multiple of 32
  *       y [.., N] = sum over k of x [.., K] times (code[n, k] - zero[n, k / G]) * scale[n, k / G].  w is U8 [N, (K + 1) / 2], two codes a
  *       byte, the even k in the low half; scale [N, groups of K] is of x's type, zero U8 of that shape (8 where it is left
- *       out).  x has rank 2 or more; 31 times the sum of a row's magnitudes is within
- *       fp32 (a row for which it is not, one with an infinity or NaN among them, may come out as NaN).  One-to-One operators, Reshapes and
- *       Splits behind the product run in its kernel, as behind MatMul. */
+ *       out).  x has rank 2 or more; 31 times the sum of a row's magnitudes is within fp32 (a row for which it is not, one with an
+ *       infinity or NaN among them, may come out as NaN; scales are finite).  One-to-One operators, Reshapes and Splits behind the
+ *       product run in its kernel, as behind MatMul. */
 dnnf_status dnnf_graph_add_op(dnnf_graph* g, const char* op_kind, int n_in, const int* in_ids, int n_out,
                               const int* out_ids, const dnnf_attr* attrs, int n_attrs, int* op_id);
 

@@ -740,3 +740,42 @@ def test_steps_below_the_normal_numbers(dtype):
     assert np.all(np.abs(got["o"][1]) <= 127 * 2.0 ** -126)
     assert np.all(np.isfinite(got["o"]))
     check_attention(spec, got)
+
+
+@pytest.mark.parametrize("how", ["held_computed", "table_gathered", "q_transposed", "all_weights", "residual", "weights_only", "weights_only_split"])
+@pytest.mark.parametrize("fusion", [0, 1])
+def test_operands_that_other_operators_make(how, fusion):
+    """Positions, tables and queries that the graph computes, and products and attention over weights alone (computed at prepare)."""
+    b = dg.GraphBuilder(how, "bf16")
+    if how in ("residual", "weights_only", "weights_only_split"):
+        K, N = (16384 if how == "weights_only_split" else 96), 96
+        x = (b.input if how == "residual" else b.weight)("x", (5, K), dg.normal(5, 1, (5, K), "bf16"))
+        w = b.weight("w", (N, K // 2), dg.rng.integers(5, 2, (N, K // 2), 0, 256), dtype="u8")
+        s = b.weight("s", (N, K // 32), dg.rng.round_to(dg.rng.uniform(5, 3, (N, K // 32), 0.01, 0.05), "bf16"))
+        y = b.op("MatMulInt4", [x, w, s], (5, N), {"group_size": 32})
+        y = b.op("Add", [y, x if how == "residual" else b.input("r", (5, N), dg.normal(5, 4, (5, N), "bf16"))], (5, N))
+    else:
+        b.g = dg.attend_graph("bf16", "bf16", [9, 40, 77])
+        op, y = b.g.ops.pop(), "o"
+        if how == "held_computed":
+            del b.g.tensors["held"]
+            op.inputs[-1] = b.op("Add", [b.input("first", (3,), np.array([8, 39, 76]), dtype="i32"), b.const("one", 1, dtype="i32")], (3,), out_dtype="i32")
+        elif how == "table_gathered":
+            t = b.g.tensors.pop("table").data
+            who = b.input("who", (3,), np.array([4, 1, 2]), dtype="i64")
+            op.inputs[-2] = b.op("Gather", [b.input("tables", (5, 8), np.concatenate([t, t[:2]]), dtype="i32"), who], (3, 8), {"axis": 0}, out_dtype="i32")
+        elif how == "q_transposed":
+            del b.g.tensors["q"]
+            op.inputs[0] = b.op("Transpose", [b.input("qt", (4, 3, 64), dg.normal(5, 1, (4, 3, 64), "bf16"))], (3, 4, 64), {"perm": [1, 0, 2]})
+        else:
+            for t in b.g.tensors.values():
+                t.kind = "weight" if t.kind == "input" else t.kind
+        b.g.ops.append(op)
+        b.g.tensors["o"].kind = "intermediate"
+        y = b.op("Add", ["o", b.input("r", (3, 4, 64), dg.normal(5, 4, (3, 4, 64), "bf16"))], (3, 4, 64))
+    b.mark_output(y)
+    spec = b.finish()
+    from parity import TOL, rel_err
+
+    _, got = run(spec, fusion=fusion)
+    assert rel_err(got[y], run_graph(spec)[y]) <= TOL["bf16"]

@@ -380,3 +380,21 @@ def test_products_and_launches_beyond_the_index_ranges():
     g.finalize()
     with pytest.raises(api.DnnfError, match="more workgroups than one launch takes"):
         api.Plan(g, [])
+
+
+def test_later_host_code_under_sanitizers(tmp_path):
+    """Plans with converting Reshapes, the write of many pages and two caches, through the instrumented library."""
+    from test_host_sanitizers import run, write_spec
+
+    from paper_2108_13342_amd import build
+
+    specs = {how: dg.cast_graph(how) for how in dg.CASTS}
+    specs.update(two=dg.two_caches_graph(), many=dg.write_graph("f32", "i8", 2049, [0, 7], [3, 2049], S=1, M=2100))
+    files = []
+    for name, spec in specs.items():
+        files.append(str(tmp_path / (name + ".txt")))
+        write_spec(spec, files[-1], expect_finalize=0)
+    r = run(build.build_sanitizer_driver(), files)
+    assert r.returncode == 0, (r.stdout[-2000:], r.stderr[-6000:])
+    assert "Sanitizer" not in r.stderr and "runtime error" not in r.stderr, r.stderr[-6000:]
+    assert r.stdout.count("\nok ") + r.stdout.startswith("ok ") == len(files), r.stdout

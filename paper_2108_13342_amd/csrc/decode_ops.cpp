@@ -78,8 +78,7 @@ CacheOperands cache_operands(const Graph& g, const Op& op) {
 }
 
 int64_t cache_positions(const Op& op, const CacheOperands& c) {
-  if (op.info->cls == OC_CACHE_WRITE) return std::min(c.T, c.M * c.S);
-  if (op.info->cls == OC_CACHE_READ) return std::min(c.T, c.M * c.S);
+  if (op.info->cls != OC_CACHE_ATTN) return std::min(c.T, c.M * c.S);
   const int64_t window = whole_attr(op, "window");
   return window > 0 ? std::min(window, c.M * c.S) : c.M * c.S;
 }
